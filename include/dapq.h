@@ -277,6 +277,96 @@ int dapq_recall(const dapq_shape* shape, const int32_t* idx_gold, const int32_t*
 int dapq_decode_attention(const dapq_shape* shape, const void* q_decode, const void* k_cache, const void* v_cache,
                           const int32_t* count, int32_t budget, float* out, void* stream);
 
+/* --- Decoding over a cache in pages ------------------------------------------------------------------------------
+ * dapq_gather and dapq_decode_attention work on a compact cache of a fixed number of rows.  The calls below hold a
+ * sequence's rows in pages of a pool instead, as bf16 or in 4 bits: the rows that the eviction kept come first
+ * (dapq_paged_gather), the rows of the tokens that are decoded, or of the conversation's next turn, follow
+ * (dapq_paged_append), and dapq_paged_attention reads them.  A row's place in the cache and its position are two
+ * things here: behind an eviction that kept 983 rows of 32768, row 983 stands for position 32768.
+ *
+ * Row i of a sequence is slot i % page_rows of page table[seq * max_pages + i / page_rows].  The layers share the table;
+ * every layer has a pool of n_pages pages of its own, one after the other.  A page holds page_rows rows of each KV head:
+ *   row number R = ((layer * n_pages + page) * n_kv_heads + head) * page_rows + slot
+ *   DAPQ_PAGES_BF16  k, v: 128 bf16 at byte 256 * R.  k_scales, v_scales are not used.
+ *   DAPQ_PAGES_FP4   k, v: 128 codes at byte 64 * R, channel c in byte c / 2, the even channel in the low four bits;
+ *                    k_scales, v_scales: 4 bytes at byte 4 * R, byte g for the channels 32g .. 32g + 31.  A code is a sign bit
+ *                    (8) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; scale byte s multiplies it by 2^(s - 127), 255 makes all 32
+ *                    NaN.  What the calls write are bf16 numbers, so nothing is rounded a second time when it is read.
+ *                    What writes a group takes the least e in [-125, 125] with max |x| <= 7 * 2^e (at which 6 is still
+ *                    a nearest level), rounds x / 2^e to the nearest level, of two the one with the even code, at most 6,
+ *                    and writes s = e + 127; a group with an infinity or a NaN gets 255 (and codes 0).
+ * An entry of the table outside [0, n_pages) is no page, and rows past max_pages * page_rows are on no page: nothing is written
+ * there, and nothing read.  Two sequences may share pages that neither call writes to. */
+enum { DAPQ_PAGES_BF16 = 0, DAPQ_PAGES_FP4 = 1 };
+typedef struct dapq_pages {
+  int32_t n_layers;
+  int32_t batch;          /* sequences of the table; dapq_paged_gather and dapq_paged_read take up to 32767 */
+  int32_t n_kv_heads;
+  int32_t head_dim;       /* 128 */
+  int32_t format;         /* DAPQ_PAGES_* */
+  int32_t page_rows;      /* rows of a page: 16, 32, 64, 128, 256, 512 or 1024 */
+  int32_t n_pages;        /* pages of a layer's pool */
+  int32_t max_pages;      /* entries of a sequence in the table; max_pages * page_rows < 2^30 */
+  void *k, *v;            /* device, the pools, 16-byte aligned */
+  void *k_scales, *v_scales;  /* device, 16-byte aligned; DAPQ_PAGES_FP4 only */
+  const int32_t* table;   /* device, [batch][max_pages] */
+} dapq_pages;
+
+/* The new tokens of a step: one for every sequence while decoding, a few that were drafted, or a whole turn; a sequence may
+ * have none.  The tokens of the batch are packed: token t of sequence seq is row cu_new[seq] + t. */
+typedef struct dapq_step {
+  int32_t n_q_heads;      /* a multiple of the pages' n_kv_heads */
+  int32_t max_new;        /* no sequence has more new tokens than this (those that it has more are left out) */
+  int64_t total_new;      /* new tokens of the batch */
+  const int32_t* cu_new;  /* device, [batch + 1], cu_new[0] = 0, non-decreasing, last = total_new;
+                             NULL = every sequence has total_new / batch */
+  const int32_t* lengths; /* device, [batch]: rows that each sequence held BEFORE these tokens (>= 0), for both calls of a
+                             step; their own rows are lengths[seq] + t */
+  int64_t k_stride_layer, k_stride_row, k_stride_head;  /* of k_new, v_new and q, in elements */
+  int64_t v_stride_layer, v_stride_row, v_stride_head;
+  int64_t q_stride_layer, q_stride_row, q_stride_head;
+  float scale;            /* 1/sqrt(d_k) */
+  float softcap;          /* 0: none; > 0: a score x becomes softcap * tanh(x / softcap) */
+} dapq_step;
+
+/* Cache pruning into pages: dapq_gather with the cache in pages as its destination.  Row i < count of KV head h of sequence
+ * seq becomes the prompt's row idx[i] of that head; FP4 pages quantise it.  shape, k, v, idx, count and budget are those of
+ * dapq_gather; the layers, the batch and the KV heads of shape and pages must be the same.  Rows past count, and rows whose index lies
+ * outside the prompt, are left as they were.  k and v must not overlap the pages. */
+int dapq_paged_gather(const dapq_shape* shape, const dapq_pages* pages, const void* k, const void* v, const int32_t* idx,
+                      const int32_t* count, int32_t budget, void* stream);
+
+/* The rows of new tokens go behind what each sequence holds: row lengths[seq] + t becomes
+ *   K: RoPE_{positions[cu_new[seq] + t]}(k_new), rounded to bf16 once as by dapq_rope_apply (FP4 pages: then quantised)
+ *   V: v_new (FP4 pages: quantised)
+ *   k_new, v_new  device, bf16, element (layer, token, head, c) at layer*stride_layer + token*stride_row + head*stride_head + c
+ *   positions     device, int32 [total_new], >= 0; NULL: the keys are stored as they are (theta, pairing unused)
+ * Uses cu_new, lengths, max_new, total_new and the K and V strides of step.  Two sequences must not append to one page. */
+int dapq_paged_append(const dapq_pages* pages, const dapq_step* step, const void* k_new, const void* v_new,
+                      const int32_t* positions, double theta, int32_t pairing, void* stream);
+
+/* Rows of a paged cache as bf16 values in the layout of the compact cache, for dapq_score (a later turn that evicts again),
+ * dapq_decode_attention, or to move a sequence elsewhere: for i < min(lengths[seq], max_rows)
+ *   k_out[layer][seq][head][i][c], v_out[...]  bf16 [n_layers][batch][n_kv_heads][max_rows][128], 16-byte aligned
+ * is row i of the sequence.  Rows of no page, and rows past lengths, are left as they were.
+ *   lengths   device, int32 [batch]: rows of each sequence */
+int dapq_paged_read(const dapq_pages* pages, const int32_t* lengths, int32_t max_rows, void* k_out, void* v_out, void* stream);
+
+/* Attention of the new tokens over the paged cache, causal among themselves (their rows have been appended): for token t of
+ * sequence seq and query head h, over the rows j <= lengths[seq] + t of KV head h / (H_q/H_kv) that are on a page,
+ *   x_j = scale * q.k_j, or softcap * tanh(scale * q.k_j / softcap);   out = sum_j softmax_j(x) v_j
+ *   q    device, bf16, rotated, element (layer, token, head, c) by the q strides of step
+ *   out  device, bf16 [n_layers][total_new][n_q_heads][128], 16-byte aligned; 0 where no row is visible
+ *   workspace  device scratch of at least dapq_paged_attention_workspace_bytes(pages, step), 256-byte aligned: sums of cache parts that
+ *        were shared out.  The figure depends on neither the lengths nor cu_new, so that a recorded call holds for all of them.
+ * Sums, maxima and weights are fp32, weights enter the product with the values as two bf16 numbers (16 bits of their
+ * significand) for up to 32 query rows of a KV head (new tokens x H_q/H_kv) and as one beyond; the result is rounded once. */
+int dapq_paged_attention(const dapq_pages* pages, const dapq_step* step, const void* q, void* out, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace dapq_paged_attention needs (0 if the arguments are invalid: the call itself then reports why). */
+size_t dapq_paged_attention_workspace_bytes(const dapq_pages* pages, const dapq_step* step);
+
 #ifdef __cplusplus
 }
 #endif

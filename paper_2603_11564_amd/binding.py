@@ -22,6 +22,7 @@ EXPORTS = (
     "dapq_workspace_bytes", "dapq_last_error", "dapq_rope_apply", "dapq_pseudo_tokens", "dapq_pseudo_queries", "dapq_pseudo_queries_workspace_bytes", "dapq_score", "dapq_score_stats",
     "dapq_score_accumulate", "dapq_score_stats_extend", "dapq_pool", "dapq_topk", "dapq_pool_topk", "dapq_topk_workspace_bytes", "dapq_gather", "dapq_recall", "dapq_decode_attention",
     "dapq_score_static", "dapq_score_static_capacity", "dapq_score_single_launch",
+    "dapq_paged_gather", "dapq_paged_append", "dapq_paged_read", "dapq_paged_attention", "dapq_paged_attention_workspace_bytes",
 )
 
 
@@ -55,6 +56,27 @@ class Qproj(C.Structure):
         ("x_stride_layer", C.c_int64), ("x_stride_token", C.c_int64),
         ("w_stride_layer", C.c_int64), ("w_stride_row", C.c_int64),
         ("q_stride_layer", C.c_int64), ("q_stride_head", C.c_int64), ("q_stride_row", C.c_int64),
+    ]
+
+
+class Pages(C.Structure):
+    """Mirror of `dapq_pages`."""
+    _fields_ = [
+        ("n_layers", C.c_int32), ("batch", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("format", C.c_int32), ("page_rows", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p), ("table", C.c_void_p),
+    ]
+
+
+class Step(C.Structure):
+    """Mirror of `dapq_step`."""
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("max_new", C.c_int32), ("total_new", C.c_int64),
+        ("cu_new", C.c_void_p), ("lengths", C.c_void_p),
+        ("k_stride_layer", C.c_int64), ("k_stride_row", C.c_int64), ("k_stride_head", C.c_int64),
+        ("v_stride_layer", C.c_int64), ("v_stride_row", C.c_int64), ("v_stride_head", C.c_int64),
+        ("q_stride_layer", C.c_int64), ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64),
+        ("scale", C.c_float), ("softcap", C.c_float),
     ]
 
 
@@ -95,18 +117,25 @@ def load_library():
     lib.dapq_score_static.argtypes = [sp, vp, vp, vp, vp]
     lib.dapq_score_static_capacity.argtypes = []
     lib.dapq_score_single_launch.argtypes = [sp]
+    pp, tp = C.POINTER(Pages), C.POINTER(Step)
+    lib.dapq_paged_gather.argtypes = [sp, pp, vp, vp, vp, vp, i32, vp]
+    lib.dapq_paged_append.argtypes = [pp, tp, vp, vp, vp, C.c_double, i32, vp]
+    lib.dapq_paged_read.argtypes = [pp, vp, i32, vp, vp, vp]
+    lib.dapq_paged_attention.argtypes = [pp, tp, vp, vp, vp, sz, vp]
+    lib.dapq_paged_attention_workspace_bytes.argtypes = [pp, tp]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = C.c_int
     lib.dapq_pseudo_queries_workspace_bytes.restype = sz
     lib.dapq_score_static_capacity.restype = sz
     lib.dapq_topk_workspace_bytes.restype = sz
+    lib.dapq_paged_attention_workspace_bytes.restype = sz
     try:
         from . import _native as native
     except ImportError as e:
         raise ImportError(f"the extension module {_PKG}/_native is not built for this Python; run "
                           "`python -m paper_2603_11564_amd.build` (there is no fallback path)") from e
     native.bind({name: C.cast(getattr(lib, name), vp).value for name in EXPORTS}, _resolve_current_stream, Shape, Qproj,
-                _through_ctypes)
+                Pages, Step, _through_ctypes)
     _native = native
     _lib = lib
     return lib
@@ -283,4 +312,56 @@ def pseudo_queries_workspace_bytes(desc) -> int:
 
 def dapq_pseudo_queries(desc, x, token_idx, w_q, positions, theta, pairing, q_out, workspace=None, stream=None):
     if rc := (_native or _calls()).pseudo_queries(desc, x, token_idx, w_q, positions, float(theta), int(pairing), q_out, workspace, stream):
+        _check(rc)
+
+
+PAGE_FORMATS = {"bf16": 0, "fp4": 1}
+
+
+def make_pages(*, n_layers, batch, n_kv_heads, page_rows, n_pages, max_pages, format, k, v, table, k_scales=None, v_scales=None,
+               head_dim=128) -> Pages:
+    """format: "bf16" or "fp4".  k, v, k_scales, v_scales: the pools; table: device int32 [batch][max_pages].  The descriptor keeps them alive."""
+    p = Pages()
+    p.n_layers, p.batch, p.n_kv_heads, p.head_dim = n_layers, batch, n_kv_heads, head_dim
+    p.format, p.page_rows, p.n_pages, p.max_pages = PAGE_FORMATS[format], page_rows, n_pages, max_pages
+    p.k, p.v, p.k_scales, p.v_scales, p.table = _ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), _ptr(table)
+    p._keepalive = (k, v, k_scales, v_scales, table)
+    return p
+
+
+def make_step(*, n_q_heads, total_new, max_new, lengths, cu_new=None, k_strides=(0, 0, 0), v_strides=(0, 0, 0), q_strides=(0, 0, 0),
+              scale, softcap=0.0) -> Step:
+    """Strides are (layer, row, head) in elements.  cu_new: device int32 tensor or None; lengths: device int32 tensor, the rows held before."""
+    s = Step()
+    s.n_q_heads, s.max_new, s.total_new = n_q_heads, max_new, total_new
+    s.cu_new, s.lengths = _ptr(cu_new), _ptr(lengths)
+    s.k_stride_layer, s.k_stride_row, s.k_stride_head = k_strides
+    s.v_stride_layer, s.v_stride_row, s.v_stride_head = v_strides
+    s.q_stride_layer, s.q_stride_row, s.q_stride_head = q_strides
+    s.scale, s.softcap = float(scale), float(softcap)
+    s._keepalive = (cu_new, lengths)
+    return s
+
+
+def dapq_paged_gather(shape, pages, k, v, idx, count, budget, stream=None):
+    if rc := (_native or _calls()).paged_gather(shape, pages, k, v, idx, count, budget, stream):
+        _check(rc)
+
+
+def dapq_paged_append(pages, step, k_new, v_new, positions, theta, pairing=0, stream=None):
+    if rc := (_native or _calls()).paged_append(pages, step, k_new, v_new, positions, float(theta), pairing, stream):
+        _check(rc)
+
+
+def dapq_paged_read(pages, lengths, max_rows, k_out, v_out, stream=None):
+    if rc := (_native or _calls()).paged_read(pages, lengths, max_rows, k_out, v_out, stream):
+        _check(rc)
+
+
+def paged_attention_workspace_bytes(pages, step) -> int:
+    return int(load_library().dapq_paged_attention_workspace_bytes(C.byref(pages), C.byref(step)))
+
+
+def dapq_paged_attention(pages, step, q, out, workspace, stream=None):
+    if rc := (_native or _calls()).paged_attention(pages, step, q, out, workspace, stream):
         _check(rc)

@@ -14,7 +14,7 @@
 namespace {
 
 PyObject *g_resolver = nullptr, *g_stream = nullptr, *g_device = nullptr;  // see stream_of
-PyTypeObject *g_shape = nullptr, *g_qproj = nullptr;                       // the descriptors' classes
+PyTypeObject *g_shape = nullptr, *g_qproj = nullptr, *g_pages = nullptr, *g_step = nullptr;  // the descriptors' classes
 PyObject* g_other_way = nullptr;                                           // see other_way
 PyObject *g_data_ptr, *g_numel, *g_element_size, *g_cuda_stream;           // interned names
 
@@ -92,6 +92,8 @@ bool stream_of(PyObject* s, void** out) {
 // A copy of a descriptor (a ctypes structure of its own class).
 PyTypeObject* class_of(const dapq_shape*) { return g_shape; }
 PyTypeObject* class_of(const dapq_qproj*) { return g_qproj; }
+PyTypeObject* class_of(const dapq_pages*) { return g_pages; }
+PyTypeObject* class_of(const dapq_step*) { return g_step; }
 template <typename T>
 bool struct_of(PyObject* v, T* out) {
   if (class_of(out) == nullptr || !PyObject_TypeCheck(v, class_of(out))) {
@@ -128,18 +130,24 @@ struct Calls {
   decltype(&dapq_decode_attention) decode_attention;
   decltype(&dapq_pseudo_tokens) pseudo_tokens;
   decltype(&dapq_pseudo_queries) pseudo_queries;
+  decltype(&dapq_paged_gather) paged_gather;
+  decltype(&dapq_paged_append) paged_append;
+  decltype(&dapq_paged_read) paged_read;
+  decltype(&dapq_paged_attention) paged_attention;
 };
 const char* const kNames[] = {"dapq_rope_apply", "dapq_score", "dapq_score_static", "dapq_score_stats", "dapq_score_accumulate",
                               "dapq_score_stats_extend", "dapq_pool", "dapq_topk", "dapq_pool_topk", "dapq_gather", "dapq_recall",
-                              "dapq_decode_attention", "dapq_pseudo_tokens", "dapq_pseudo_queries"};
+                              "dapq_decode_attention", "dapq_pseudo_tokens", "dapq_pseudo_queries", "dapq_paged_gather", "dapq_paged_append",
+                              "dapq_paged_read", "dapq_paged_attention"};
 constexpr int kCalls = (int)(sizeof(kNames) / sizeof(kNames[0]));
 static_assert(sizeof(Calls) == kCalls * sizeof(void*), "a name for every function");
 Calls g_calls = {};
 
-// (addresses by name, resolver of the current stream, Shape, Qproj, the way through ctypes)
+// (addresses by name, resolver of the current stream, Shape, Qproj, Pages, Step, the way through ctypes)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!count_is(n, 5)) return nullptr;
-  if (!PyType_Check(a[2]) || !PyType_Check(a[3])) return PyErr_Format(PyExc_TypeError, "classes expected");
+  if (!count_is(n, 7)) return nullptr;
+  for (int i = 2; i < 6; ++i)
+    if (!PyType_Check(a[i])) return PyErr_Format(PyExc_TypeError, "classes expected");
   void* at[kCalls];
   for (int i = 0; i < kCalls; ++i) {
     PyObject* v = PyDict_Check(a[0]) ? PyDict_GetItemString(a[0], kNames[i]) : nullptr;
@@ -150,12 +158,13 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   __builtin_memcpy(&g_calls, at, sizeof(at));
   Py_INCREF(a[1]);
   Py_XSETREF(g_resolver, a[1]);
-  Py_INCREF(a[2]);
-  Py_XSETREF(g_shape, reinterpret_cast<PyTypeObject*>(a[2]));
-  Py_INCREF(a[3]);
-  Py_XSETREF(g_qproj, reinterpret_cast<PyTypeObject*>(a[3]));
-  Py_INCREF(a[4]);
-  Py_XSETREF(g_other_way, a[4]);
+  PyTypeObject** const classes[] = {&g_shape, &g_qproj, &g_pages, &g_step};
+  for (int i = 0; i < 4; ++i) {
+    Py_INCREF(a[2 + i]);
+    Py_XSETREF(*classes[i], reinterpret_cast<PyTypeObject*>(a[2 + i]));
+  }
+  Py_INCREF(a[6]);
+  Py_XSETREF(g_other_way, a[6]);
   Py_CLEAR(g_stream);
   Py_CLEAR(g_device);
   Py_RETURN_NONE;
@@ -299,10 +308,45 @@ PyObject* pseudo_queries(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return without_lock([&] { return g_calls.pseudo_queries(&d, p[1], IP(2), p[3], IP(4), theta, I32(6), p[7], p[8], bytes, p[9]); });
 }
 
+PyObject* paged_gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ARGS(8);
+  dapq_shape s;
+  dapq_pages g;
+  if (!(struct_of(a[0], &s) && struct_of(a[1], &g) && P(2) && P(3) && P(4) && P(5) && I(6) && stream_of(a[7], &p[7])))
+    return other_way("dapq_paged_gather", a, n);
+  return without_lock([&] { return g_calls.paged_gather(&s, &g, p[2], p[3], IP(4), IP(5), I32(6), p[7]); });
+}
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ARGS(8);
+  dapq_pages g;
+  dapq_step t;
+  if (!(struct_of(a[0], &g) && struct_of(a[1], &t) && P(2) && P(3) && P(4) && I(6) && stream_of(a[7], &p[7])))
+    return other_way("dapq_paged_append", a, n);
+  const double theta = PyFloat_AsDouble(a[5]);
+  if (PyErr_Occurred()) return nullptr;
+  return without_lock([&] { return g_calls.paged_append(&g, &t, p[2], p[3], IP(4), theta, I32(6), p[7]); });
+}
+PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ARGS(6);
+  dapq_pages g;
+  if (!(struct_of(a[0], &g) && P(1) && I(2) && P(3) && P(4) && stream_of(a[5], &p[5]))) return other_way("dapq_paged_read", a, n);
+  return without_lock([&] { return g_calls.paged_read(&g, IP(1), I32(2), p[3], p[4], p[5]); });
+}
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ARGS(6);
+  dapq_pages g;
+  dapq_step t;
+  size_t bytes;
+  if (!(struct_of(a[0], &g) && struct_of(a[1], &t) && P(2) && P(3) && P(4) && bytes_of(a[4], &bytes) && stream_of(a[5], &p[5])))
+    return other_way("dapq_paged_attention", a, n);
+  return without_lock([&] { return g_calls.paged_attention(&g, &t, p[2], p[3], p[4], bytes, p[5]); });
+}
+
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ENTRY(bind), ENTRY(rope_apply), ENTRY(score), ENTRY(score_static), ENTRY(score_stats), ENTRY(score_accumulate),
                           ENTRY(score_stats_extend), ENTRY(pool), ENTRY(topk), ENTRY(pool_topk), ENTRY(gather), ENTRY(recall),
-                          ENTRY(decode_attention), ENTRY(pseudo_tokens), ENTRY(pseudo_queries), {nullptr, nullptr, 0, nullptr}};
+                          ENTRY(decode_attention), ENTRY(pseudo_tokens), ENTRY(pseudo_queries), ENTRY(paged_gather), ENTRY(paged_append),
+                          ENTRY(paged_read), ENTRY(paged_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "calls of libdapq with torch tensors", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
