@@ -1,6 +1,9 @@
 // Attention of a step's tokens over a cache in pages.
 #include <math.h>
 
+#include <type_traits>
+
+#include "kernel_args.h"
 #include "paged.h"
 
 namespace dapq {
@@ -12,7 +15,10 @@ struct PagedAttentionParams {
   uint16_t* out;
   const int32_t *cu_new, *lengths;
   int64_t q_stride_layer, q_stride_row, q_stride_head;
+  float* parts;  // of the workspace
   int32_t batch, total_new, each_new, max_new, n_q_heads;
+  int32_t group, items, groups;  // query heads of a KV head; layers * Hkv; workgroups of the row kernel
+  float inv_group, c, cap;       // c: scale * log2(e), with a cap scale / softcap; cap: softcap * log2(e)
   float scale, softcap;
 };
 
@@ -88,6 +94,532 @@ __global__ __launch_bounds__(64) void paged_attention_kernel(PagedAttentionParam
   *reinterpret_cast<bf16x2*>(p.out + (((int64_t)layer * p.total_new + r) * p.n_q_heads + h) * kHeadDim + 2 * lane) = result;
 }
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 32;              // cache rows that a wave takes at a time
+constexpr int kRowWaves = 4;           // of a workgroup of the row kernel
+constexpr float kHeadroom = 4.0f;      // binades that a logit may lie above the reference of its column
+constexpr float kLowest = -3.4028234663852886e38f;  // where references start: finite, a logit of -inf then weighs 0
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---- how the row kernel shares out the rows ---------------------------------------------------------------------------
+// An item is one KV head of one sequence and layer, with all columns (new tokens x query heads of the KV head).  The tiles of all items, sequence by
+// sequence, are one axis; every workgroup has the same length of it, so that sequences of any lengths share the chip evenly.  An
+// item that lies in one workgroup is finished there; the parts of the others meet in a second kernel, in order.
+struct Sequence {
+  int first, tokens;  // its new tokens
+  int before;         // rows held before them
+  int tiles;          // of an item; 0 if it has no new tokens
+};
+
+// The rows that token t sees.
+__device__ __forceinline__ int rows_seen(const PagedAttentionParams& p, int before, int t) {
+  const int64_t most = (int64_t)p.pool.max_pages << p.pool.page_shift, n = (int64_t)before + t + 1;
+  return (int)(n < 0 ? 0 : (n < most ? n : most));
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Sequence sequence(const PagedAttentionParams& p, int b) {
+  Sequence s;
+  s.first = p.cu_new == nullptr ? b * p.each_new : p.cu_new[b];
+  s.tokens = p.cu_new == nullptr ? p.each_new : p.cu_new[b + 1] - s.first;
+  s.tokens = s.tokens < p.max_new ? s.tokens : p.max_new;
+  s.before = p.lengths[b];
+  s.tiles = 0;
+  if (s.tokens > 0) {
+    const int n = rows_seen(p, s.before, s.tokens - 1);
+    s.tiles = n > kTile ? (n + kTile - 1) / kTile : 1;  // (an item without rows has its zeros to write)
+  }
+  return s;
+}
+// The same in all lanes.
+__device__ __forceinline__ Sequence uniform_sequence(const PagedAttentionParams& p, int b) {
+  Sequence s = sequence(p, b);
+  return {uniform(s.first), uniform(s.tokens), uniform(s.before), uniform(s.tiles)};
+}
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+// The tiles of the sequences, 64 sequences at a time, one to a lane.
+template <typename F>
+__device__ __forceinline__ void walk_axis(const PagedAttentionParams& p, int lane, F each) {
+  int64_t before = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 64) {
+    int64_t n = b0 + lane < p.batch ? (int64_t)sequence(p, b0 + lane).tiles * p.items : 0;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t o = __shfl_up(n, d, 64);
+      if (lane >= d) n += o;
+    }
+    each(b0, before, n);  // n: tiles up to and with this lane's sequence, in this block of 64
+    before += uniform64(__shfl(n, 63, 64));
+  }
+}
+__device__ __forceinline__ int64_t tiles_of_all(const PagedAttentionParams& p, int lane) {
+  int64_t total = 0;
+  walk_axis(p, lane, [&](int, int64_t before, int64_t n) { total = before + uniform64(__shfl(n, 63, 64)); });
+  return total;
+}
+// A workgroup's length of the axis: at least a tile to a wave.
+__device__ __forceinline__ int64_t share_of(const PagedAttentionParams& p, int64_t total) {
+  const int64_t share = (total + p.groups - 1) / p.groups;
+  return share < kRowWaves ? kRowWaves : share;
+}
+
+// A part of an item in the workspace: weighted sums, references and sums of weights of its columns.
+template <int COLS>
+struct Part {
+  static constexpr int kFloats = COLS * (kHeadDim + 2);
+};
+
+// Whether one of the two bf16 of a dword is.
+__device__ __forceinline__ bool not_finite(unsigned x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+
+// log2 of a weight before the reference is taken off: c * logit, or with a cap cap * log2(e) * tanh(logit * scale / cap).
+template <bool CAP>
+__device__ __forceinline__ float capped(const PagedAttentionParams& p, float d) {
+  if constexpr (!CAP) return d;  // (times p.c where it is used)
+  // tanh(z) = 1 - 2 / (1 + exp(2 z)) loses what z is smaller than 1 by: below 1/4 the series, whose first term left out is below 2^-22 z
+  const float z = d * p.c;
+  const float big = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * (2.0f * kLog2e))), 1.0f);
+  const float u = z * z;
+  const float small = z * fmaf(u, fmaf(u, fmaf(u, fmaf(u, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+  return p.cap * (fabsf(z) < 0.25f ? small : big);
+}
+
+// One wave per 32 rows at a time, the waves of a workgroup in turn over a part of an item; both products on v_mfma_f32_16x16x32_bf16.
+//   logits   D[row][column] = K (A operand, 16 rows x 32 channels) x q (B operand); a lane has four rows of one column.
+//   weights  2^(c * logit - ref) in fp32; ref only moves, and the sums are rescaled, where a logit lies more than kHeadroom binades above it.
+//   output   D[column][channel] += weights (A) x V (B); a weight enters as two bf16 numbers, the leading 8 bits of its significand and the next 8.
+//            V is transposed in registers: a lane loads the same 8 channels of 8 rows.
+// BLOCKS: blocks of 16 columns; 0: up to 8 columns, whose leading and following parts take the two halves of one block.
+template <bool FP4, int BLOCKS, bool CAP>
+__global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAttentionParams p) {
+  constexpr bool kHalf = BLOCKS == 0;
+  constexpr int NB = kHalf ? 1 : BLOCKS, kCols = kHalf ? 8 : 16 * BLOCKS;
+  constexpr int kWaveFloats = NB * 16 * (kHeadDim + 2);
+  constexpr bool kQueriesInLds = NB == 2;  // (there are no registers for them)
+  constexpr bool kLate = NB == 2 && !FP4;  // the next keys are loaded where registers are left for them
+  static_assert(!kQueriesInLds || kRowWaves == 4, "a wave brings in half a block");
+  extern __shared__ float lds[];  // [waves]: weighted sums, references, sums of weights; queries
+  bf16x8* queries = reinterpret_cast<bf16x8*>(lds + kRowWaves * kWaveFloats);
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  float* mine = lds + wave * kWaveFloats;
+  const int g = p.group;
+
+  // this workgroup's part of the axis, and the sequence it starts in
+  const int64_t share = share_of(p, tiles_of_all(p, lane));
+  const int64_t from = (int64_t)blockIdx.x * share;
+  int seq = p.batch;
+  int64_t seq_from = 0;
+  walk_axis(p, lane, [&](int b0, int64_t before, int64_t tiles) {
+    const uint64_t past = __ballot(before + tiles > from);
+    if (seq == p.batch && past != 0) {
+      const int at = __builtin_ctzll(past);
+      seq = b0 + at;
+      seq_from = before + (at > 0 ? uniform64(__shfl(tiles, at > 0 ? at - 1 : 0, 64)) : 0);
+    }
+  });
+  if (seq >= p.batch) return;
+  int64_t left = uniform64(share);
+  seq = uniform(seq);
+  Sequence s = uniform_sequence(p, seq);
+  int item = uniform((int)((from - seq_from) / s.tiles));  // layer * Hkv + head
+  int tile0 = uniform((int)((from - seq_from) - (int64_t)item * s.tiles));
+
+  while (left > 0) {
+    const int tile1 = uniform(s.tiles - tile0 < left ? s.tiles : tile0 + (int)left);
+    const int layer = item / p.pool.n_kv_heads, head = item - layer * p.pool.n_kv_heads;
+    const int cols = s.tokens * g;
+    // the columns of this lane: query rows as operand, and what they see
+    bf16x8 qf[kQueriesInLds ? 1 : NB][4];
+    int vis[NB];
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+      int col = kHalf ? n & 7 : 16 * t + n;
+      col = col < cols ? col : cols - 1;
+      const int token = quotient(col, p.inv_group), h = head * g + col - token * g;
+      vis[t] = rows_seen(p, s.before, token);
+      const uint16_t* src = p.q + layer * p.q_stride_layer + (int64_t)(s.first + token) * p.q_stride_row + (int64_t)h * p.q_stride_head;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (kQueriesInLds && 2 * t + (i >> 1) != wave) continue;
+        const bf16x8 x = *reinterpret_cast<const bf16x8*>(src + (FP4 ? 32 * kg + 8 * i : 32 * i + 8 * kg));
+        if constexpr (kQueriesInLds) queries[(t * 4 + i) * 64 + lane] = x;
+        else qf[t][i] = x;
+      }
+    }
+    if (kQueriesInLds) __syncthreads();
+    const int seen_by_all = rows_seen(p, s.before, 0), seen_by_last = rows_seen(p, s.before, s.tokens - 1);
+
+    // pages of this wave's tiles, 64 tiles at a time, one to a lane
+    const int32_t* table = p.pool.table + (int64_t)seq * p.pool.max_pages;
+    int page0 = -1, page1 = -1;
+    auto load_pages = [&](int k) {
+      int l = lane;
+      asm volatile("" : "+v"(l));
+      const int64_t tile = (int64_t)tile0 + wave + (int64_t)kRowWaves * (k + l);
+      page0 = page1 = -1;
+      if (tile < tile1) {
+        const int64_t e0 = tile * kTile >> p.pool.page_shift, e1 = (tile * kTile + 16) >> p.pool.page_shift;
+        page0 = e0 < p.pool.max_pages ? table[e0] : -1;
+        page1 = e1 < p.pool.max_pages ? table[e1] : -1;
+        if (page0 >= p.pool.n_pages) page0 = -1;
+        if (page1 >= p.pool.n_pages) page1 = -1;
+      }
+    };
+    struct Rows {
+      int64_t at[2];  // row numbers of the two halves of a tile (of page 0 where they are on no page)
+      bool ok[2];
+    };
+    auto rows_of = [&](int k) {
+      if ((k & 63) == 0) load_pages(k);
+      Rows r;
+      const int64_t tile = (int64_t)tile0 + wave + (int64_t)kRowWaves * k;
+      const int pa = __builtin_amdgcn_readlane(page0, k & 63), pb = __builtin_amdgcn_readlane(page1, k & 63);
+      const int slot = (int)(tile * kTile) & ((1 << p.pool.page_shift) - 1), slot1 = (int)(tile * kTile + 16) & ((1 << p.pool.page_shift) - 1);
+      r.ok[0] = pa >= 0;
+      r.ok[1] = pb >= 0;
+      r.at[0] = uniform64(page_row(p.pool, layer, pa < 0 ? 0 : pa, head) + slot);
+      r.at[1] = uniform64(page_row(p.pool, layer, pb < 0 ? 0 : pb, head) + slot1);
+      return r;
+    };
+    // A tile in registers.  Keys: the operand (bf16), or a row's group of 32 channels to a lane.  Values: 8 channels of the rows
+    // 16 * (e / 4) + 4 * kg + e % 4.
+    u32x4 kf[2][FP4 ? 1 : 4];
+    unsigned ks[2];
+    u32x4 vt[FP4 ? 1 : 8];
+    unsigned vc[8];
+    u32x4 vs[2];
+    // (through descriptors of 16 rows each: the address of a lane is an offset of 32 bits)
+    const unsigned k_at = n * (FP4 ? kFp4RowBytes : kRowBytes) + kg * 16, v_at = 4 * kg * (FP4 ? kFp4RowBytes : kRowBytes) + n * (FP4 ? 4 : 16);
+    auto rows16 = [&](uint8_t* pool, int64_t at, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(pool + at * bytes, 0, 16 * bytes, 0x00020000); };
+    auto load_k = [&](const Rows& r) {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const auto src = rows16(p.pool.k, r.at[hf], FP4 ? kFp4RowBytes : kRowBytes);
+#pragma unroll
+        for (int i = 0; i < (FP4 ? 1 : 4); ++i) kf[hf][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)k_at + i * 64, 0, 0));
+        if constexpr (FP4) ks[hf] = __builtin_amdgcn_raw_buffer_load_b8(rows16(p.pool.k_scales, r.at[hf], 4), n * 4 + kg, 0, 0);
+      }
+    };
+    auto load_v = [&](const Rows& r) {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const auto src = rows16(p.pool.v, r.at[hf], FP4 ? kFp4RowBytes : kRowBytes);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (FP4) vc[4 * hf + e] = __builtin_amdgcn_raw_buffer_load_b32(src, (int)v_at + e * kFp4RowBytes, 0, 0);
+          else vt[4 * hf + e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)v_at + e * kRowBytes, 0, 0));
+        }
+        if constexpr (FP4) vs[hf] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows16(p.pool.v_scales, r.at[hf], 4), 16 * kg, 0, 0));
+      }
+    };
+
+    f32x4 acc[NB][8];
+    float ref[NB], sum[NB];
+    bool seen[NB];  // (by this lane's rows)
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[t][j] = {0.0f, 0.0f, 0.0f, 0.0f};
+      ref[t] = kLowest;
+      sum[t] = 0.0f;
+      seen[t] = false;
+    }
+
+    bool apart = false;  // whether there are such values
+    Rows now = {};
+    if (tile0 + wave < tile1) {
+      now = rows_of(0);
+      load_k(now);
+      load_v(now);
+    }
+    for (int k = 0; tile0 + wave + kRowWaves * k < tile1; ++k) {
+      const int row0 = (tile0 + wave + kRowWaves * k) * kTile;
+      const bool more = tile0 + wave + kRowWaves * (k + 1) < tile1;
+      const bool partial = row0 + kTile > seen_by_all || !now.ok[0] || !now.ok[1];
+      float xs[NB][8];
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        f32x4 d[NB];
+#pragma unroll
+        for (int t = 0; t < NB; ++t) d[t] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u32x4 a;
+          if constexpr (FP4) a = fp4_unpack8(kf[hf][0][i], fp4_scale(ks[hf]));
+          else a = kf[hf][i];
+#pragma unroll
+          for (int t = 0; t < NB; ++t)
+            d[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), kQueriesInLds ? queries[(t * 4 + i) * 64 + lane] : qf[kQueriesInLds ? 0 : t][i], d[t], 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < NB; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) xs[t][4 * hf + v] = capped<CAP>(p, d[t][v]);
+      }
+      Rows next = now;
+      if (more) {
+        next = rows_of(k + 1);
+        if (!kLate) load_k(next);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      u32x4 hi[NB], lo[NB];  // the weights as A operand
+#pragma unroll
+      for (int t = 0; t < NB; ++t) {
+        float(&x)[8] = xs[t];
+        if (partial) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool there = row0 + 16 * (e >> 2) + 4 * kg + (e & 3) < vis[t] && now.ok[e >> 2];
+            seen[t] |= there;
+            if (!there) x[e] = -INFINITY;
+          }
+        } else {
+          seen[t] = true;
+        }
+        float m = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) m = fmaxf(m, x[e]);
+        if (!CAP) m *= p.c;
+        if (__any(m > ref[t] + kHeadroom)) {
+          m = fmaxf(m, __shfl_xor(m, 16, 64));
+          m = fmaxf(m, __shfl_xor(m, 32, 64));
+          const float moved = fmaxf(ref[t], m);
+          const float f = __builtin_amdgcn_exp2f(ref[t] - moved);
+          ref[t] = moved;
+          sum[t] *= f;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float fv = __shfl(f, 4 * kg + v, 64);  // (row 4 * kg + v of the sums is column 4 * kg + v)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[t][j][v] *= fv;
+          }
+        }
+        unsigned w[8], w2[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float y = __builtin_amdgcn_exp2f(CAP ? x[e] - ref[t] : fmaf(x[e], p.c, -ref[t]));
+          sum[t] += y;
+          // what the leading part leaves, and 2^-22 of the weight, which keeps it from 0 where a value is infinite
+          const float rest = fmaf(y, 1.0f + 0x1p-22f, -__uint_as_float(__float_as_uint(y) & 0xffff0000u));
+          w[e] = __float_as_uint(kHalf && n >= 8 ? rest : y);
+          w2[e] = __float_as_uint(rest);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          hi[t][e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], 0x07060302u);
+          lo[t][e] = __builtin_amdgcn_perm(w2[2 * e + 1], w2[2 * e], 0x07060302u);
+        }
+      }
+      u32x4 vr[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (FP4) vr[e] = fp4_unpack8(vc[e], fp4_scale((vs[e >> 2][e & 3] >> (8 * (n >> 2))) & 255u));
+        else vr[e] = vt[e];
+      }
+      if (partial) {
+        // Rows that no column sees may hold anything, and 0 times it must be 0.  A value that is infinite or no number, in a row that some columns
+        // see and others don't, is added to the former by itself (in LDS: sums of such values are what they are in any order).
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int row = row0 + 16 * (e >> 2) + 4 * kg + (e & 3);
+          if (row >= seen_by_last || !now.ok[e >> 2]) vr[e] = u32x4{0, 0, 0, 0};
+          if (row >= seen_by_all) odd |= not_finite(vr[e][0]) || not_finite(vr[e][1]) || not_finite(vr[e][2]) || not_finite(vr[e][3]);
+        }
+        if (__any(odd)) {
+          int n8 = 8 * n, row4 = row0 + 4 * kg;
+          asm volatile("" : "+v"(n8), "+v"(row4));  // (nothing of this is to be kept in registers outside)
+          if (!apart) {
+            for (int i = lane; i < kCols * kHeadDim; i += 64) mine[i] = 0.0f;
+            apart = true;
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int row = row4 + 16 * (e >> 2) + (e & 3);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const unsigned all = vr[e][i];
+              const unsigned bad = row >= seen_by_all ? all & (((all & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((all & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u)) : 0u;
+              vr[e][i] = all & ~bad;
+              if (bad == 0) continue;
+#pragma unroll 1
+              for (int col = 0; col < cols; ++col) {
+                if (row >= rows_seen(p, s.before, quotient(col, p.inv_group))) continue;
+                atomicAdd(mine + col * kHeadDim + n8 + 2 * i, __uint_as_float(bad << 16));
+                atomicAdd(mine + col * kHeadDim + n8 + 2 * i + 1, __uint_as_float(bad & 0xffff0000u));
+              }
+            }
+          }
+        }
+      }
+      if (kLate && more) load_k(next);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {  // channels 8 * n + j
+        u32x4 vb;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vb[e] = __builtin_amdgcn_perm(vr[2 * e + 1][j >> 1], vr[2 * e][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+        for (int t = 0; t < NB; ++t) {
+          acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi[t]), __builtin_bit_cast(bf16x8, vb), acc[t][j], 0, 0, 0);
+          if constexpr (!kHalf)
+            acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo[t]), __builtin_bit_cast(bf16x8, vb), acc[t][j], 0, 0, 0);
+        }
+      }
+      if (more) load_v(next);
+      __builtin_amdgcn_sched_barrier(0);
+      now = next;
+    }
+
+    // what the waves have, in LDS
+    if (apart) {
+#pragma unroll
+      for (int t = 0; t < NB; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[t][j][v] += mine[(kHalf ? (4 * kg + v) & 7 : 16 * t + 4 * kg + v) * kHeadDim + 8 * n + j];
+    }
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+      float w = sum[t];
+      w += __shfl_xor(w, 16, 64);
+      w += __shfl_xor(w, 32, 64);
+      const uint64_t any = __ballot(seen[t]);
+      const bool column = (any >> n | any >> (n + 16) | any >> (n + 32) | any >> (n + 48)) & 1;
+      if (kg == 0) {
+        mine[NB * 16 * kHeadDim + 16 * t + n] = column ? ref[t] : -INFINITY;  // (no row was seen)
+        mine[NB * 16 * (kHeadDim + 1) + 16 * t + n] = w;
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        f32x4* dst = reinterpret_cast<f32x4*>(mine + (16 * t + 4 * kg + v) * kHeadDim + 8 * n);
+        dst[0] = f32x4{acc[t][0][v], acc[t][1][v], acc[t][2][v], acc[t][3][v]};
+        dst[1] = f32x4{acc[t][4][v], acc[t][5][v], acc[t][6][v], acc[t][7][v]};
+      }
+    }
+    __syncthreads();
+    const bool whole = tile0 == 0 && tile1 == s.tiles;
+    float* part = p.parts + ((int64_t)blockIdx.x * 2 + (tile0 == 0 ? 1 : 0)) * Part<kCols>::kFloats;
+    int e0 = tid;
+    asm volatile("" : "+v"(e0));  // (as above: no registers for this during the loop)
+    for (int e = e0; e < cols * (kHeadDim / 2); e += 64 * kRowWaves) {
+      const int col = e / (kHeadDim / 2), c = 2 * (e % (kHeadDim / 2));
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kRowWaves; ++w) m = fmaxf(m, lds[w * kWaveFloats + NB * 16 * kHeadDim + col]);
+      f32x2 o = {0.0f, 0.0f};
+      float total = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kRowWaves; ++w) {  // (in order)
+        const float* from_wave = lds + w * kWaveFloats;
+        const float r = from_wave[NB * 16 * kHeadDim + col];
+        const float f = r == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r - m);
+        f32x2 x = *reinterpret_cast<const f32x2*>(from_wave + col * kHeadDim + c);
+        if constexpr (kHalf) x += *reinterpret_cast<const f32x2*>(from_wave + (col + 8) * kHeadDim + c);
+        if (r != -INFINITY) {
+          o[0] = fmaf(f, x[0], o[0]);
+          o[1] = fmaf(f, x[1], o[1]);
+          total = fmaf(f, from_wave[NB * 16 * (kHeadDim + 1) + col], total);
+        }
+      }
+      if (whole) {
+        const int token = quotient(col, p.inv_group), h = head * g + col - token * g;
+        bf16x2 result;
+        result[0] = (__bf16)(m == -INFINITY ? 0.0f : o[0] / total);
+        result[1] = (__bf16)(m == -INFINITY ? 0.0f : o[1] / total);
+        *reinterpret_cast<bf16x2*>(p.out + (((int64_t)layer * p.total_new + s.first + token) * p.n_q_heads + h) * kHeadDim + c) = result;
+      } else {
+        *reinterpret_cast<f32x2*>(part + col * kHeadDim + c) = o;
+        if (c == 0) {
+          part[kCols * kHeadDim + col] = m;
+          part[kCols * (kHeadDim + 1) + col] = total;
+        }
+      }
+    }
+    left = uniform64(left - (tile1 - tile0));
+    tile0 = 0;
+    if (++item == p.items) {
+      item = 0;
+      do {
+        if (++seq >= p.batch) return;
+        s = uniform_sequence(p, seq);
+      } while (s.tiles == 0);
+    }
+    __syncthreads();
+  }
+}
+
+// The items that several workgroups share: their parts, in order.  A workgroup per item.
+template <int COLS>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttentionParams p) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int seq = blockIdx.x / p.items, item = blockIdx.x - seq * p.items;
+  const Sequence s = sequence(p, seq);
+  if (s.tiles == 0) return;
+  int64_t total = 0, from = 0;
+  walk_axis(p, lane, [&](int b0, int64_t before, int64_t n) {
+    total = before + uniform64(__shfl(n, 63, 64));
+    if (seq >= b0 && seq < b0 + 64) from = before + (seq > b0 ? uniform64(__shfl(n, seq > b0 ? seq - b0 - 1 : 0, 64)) : 0);
+  });
+  const int64_t share = share_of(p, total);
+  from += (int64_t)item * s.tiles;
+  const int64_t first = from / share, last = (from + s.tiles - 1) / share;
+  if (first == last) return;
+  const int layer = item / p.pool.n_kv_heads, head = item - layer * p.pool.n_kv_heads;
+  for (int e = tid; e < s.tokens * p.group * (kHeadDim / 2); e += 256) {
+    const int col = e / (kHeadDim / 2), c = 2 * (e % (kHeadDim / 2));
+    auto part = [&](int64_t w) { return p.parts + (w * 2 + (w == first ? 1 : 0)) * Part<COLS>::kFloats; };
+    float m = -INFINITY;
+    for (int64_t w = first; w <= last; ++w) m = fmaxf(m, part(w)[COLS * kHeadDim + col]);
+    f32x2 o = {0.0f, 0.0f};
+    float sum = 0.0f;
+    for (int64_t w = first; w <= last; ++w) {
+      const float r = part(w)[COLS * kHeadDim + col];
+      if (r == -INFINITY) continue;
+      const float f = __builtin_amdgcn_exp2f(r - m);
+      const f32x2 x = *reinterpret_cast<const f32x2*>(part(w) + col * kHeadDim + c);
+      o[0] = fmaf(f, x[0], o[0]);
+      o[1] = fmaf(f, x[1], o[1]);
+      sum = fmaf(f, part(w)[COLS * (kHeadDim + 1) + col], sum);
+    }
+    const int token = quotient(col, p.inv_group), h = head * p.group + col - token * p.group;
+    bf16x2 result;
+    result[0] = (__bf16)(m == -INFINITY ? 0.0f : o[0] / sum);
+    result[1] = (__bf16)(m == -INFINITY ? 0.0f : o[1] / sum);
+    *reinterpret_cast<bf16x2*>(p.out + (((int64_t)layer * p.total_new + s.first + token) * p.n_q_heads + h) * kHeadDim + c) = result;
+  }
+}
+
+// Workgroups of the row kernel: as many as the chip holds at a time, and no more than there is work for.
+int row_groups(const dapq_pages* p) {
+  const int64_t most = (((int64_t)p->max_pages * p->page_rows + kTile - 1) / kTile) * p->n_layers * p->batch * p->n_kv_heads;
+  const int64_t groups = (most + kRowWaves - 1) / kRowWaves;
+  return (int)(groups < 512 ? groups : 512);
+}
+constexpr int kMostRowCols = 32;
+int row_cols(int64_t cols) { return cols <= 8 ? 8 : (cols <= 16 ? 16 : 32); }
+
+template <bool FP4, int BLOCKS>
+int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, hipStream_t stream) {
+  constexpr int kCols = BLOCKS == 0 ? 8 : 16 * BLOCKS, kBytes = kRowWaves * (BLOCKS == 0 ? 1 : BLOCKS) * 16 * (kHeadDim + 2) * 4 + (BLOCKS == 2 ? 8192 : 0);
+  auto kernel = p.cap > 0.0f ? paged_rows_kernel<FP4, BLOCKS, true> : paged_rows_kernel<FP4, BLOCKS, false>;
+  const int rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), kBytes);
+  if (rc != DAPQ_OK) return rc;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)p.groups), dim3(64 * kRowWaves), kBytes, stream, p);
+  DAPQ_HIP_LAUNCH_CHECK("paged_rows_kernel");
+  hipLaunchKernelGGL((paged_join_kernel<kCols>), dim3((unsigned)((int64_t)pages->batch * p.items)), dim3(256), 0, stream, p);
+  DAPQ_HIP_LAUNCH_CHECK("paged_join_kernel");
+  return DAPQ_OK;
+}
+template <bool FP4>
+int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, int cols, hipStream_t stream) {
+  return cols == 8 ? launch_rows<FP4, 0>(pages, p, stream) : (cols == 16 ? launch_rows<FP4, 1>(pages, p, stream) : launch_rows<FP4, 2>(pages, p, stream));
+}
+
 int check_attention(const dapq_pages* pages, const dapq_step* step) {
   int rc = check_pages(pages);
   if (rc == DAPQ_OK) rc = check_step(pages, step);
@@ -107,7 +639,10 @@ int check_attention(const dapq_pages* pages, const dapq_step* step) {
 using namespace dapq;
 
 extern "C" DAPQ_API size_t dapq_paged_attention_workspace_bytes(const dapq_pages* pages, const dapq_step* step) {
-  return check_attention(pages, step) == DAPQ_OK ? 256 : 0;
+  if (check_attention(pages, step) != DAPQ_OK) return 0;
+  const int64_t cols = (int64_t)step->max_new * (step->n_q_heads / pages->n_kv_heads);
+  if (cols > kMostRowCols) return 256;
+  return align_up((size_t)row_groups(pages) * 2 * row_cols(cols) * (kHeadDim + 2) * sizeof(float), 256);
 }
 
 extern "C" DAPQ_API int dapq_paged_attention(const dapq_pages* pages, const dapq_step* step, const void* q, void* out, void* workspace,
@@ -136,6 +671,17 @@ extern "C" DAPQ_API int dapq_paged_attention(const dapq_pages* pages, const dapq
   p.n_q_heads = step->n_q_heads;
   p.scale = step->scale;
   p.softcap = step->softcap;
+  p.parts = static_cast<float*>(workspace);
+  p.group = step->n_q_heads / pages->n_kv_heads;
+  p.items = pages->n_layers * pages->n_kv_heads;
+  p.groups = row_groups(pages);
+  p.inv_group = 1.0f / (float)p.group;
+  p.cap = step->softcap * kLog2e;
+  p.c = step->softcap > 0.0f ? step->scale / step->softcap : step->scale * kLog2e;
+  const int64_t cols = (int64_t)step->max_new * p.group;
+  if (cols <= kMostRowCols)
+    return pages->format == DAPQ_PAGES_FP4 ? launch_rows<true>(pages, p, row_cols(cols), static_cast<hipStream_t>(stream))
+                                           : launch_rows<false>(pages, p, row_cols(cols), static_cast<hipStream_t>(stream));
   hipLaunchKernelGGL(pages->format == DAPQ_PAGES_FP4 ? paged_attention_kernel<true> : paged_attention_kernel<false>,
                      dim3((unsigned)step->total_new, (unsigned)step->n_q_heads, (unsigned)pages->n_layers), dim3(64), 0,
                      static_cast<hipStream_t>(stream), p);

@@ -270,6 +270,28 @@ def test_attention_of_no_numbers():
     assert nan[0, 2:10, :2].all() and not nan[0, :2].any() and not nan[0, 10:].any() and not nan[0, :, 2:].any()
 
 
+@pytest.mark.parametrize("group,new", [(1, 1), (4, 1), (2, 3), (8, 2), (4, 7), (2, 60)])
+def test_values_that_are_not_finite(group, new):
+    """An infinite value or a NaN among the values of the new tokens reaches the tokens from its own on; what nobody sees reaches nobody."""
+    rng = np.random.default_rng(60 + new)
+    before = 45
+    cache = Cache(rng, "bf16", 1, 2, 16, [before + new + 30]).fill(rng, [before + new])
+    plant = {5: (0, np.inf), 20: (1, np.nan), before: (2, -np.inf), before + new // 2: (3, np.nan), before + new - 1: (4, np.inf)}
+    for row, (channel, value) in plant.items():
+        page, slot = PO.place(cache.table, cache.n_pages, 16, 0, row)
+        cache.pool["v"][0, page, 1, slot, channel] = O.f64_to_bf16_bits(np.array([value]))[0]
+    cache.to_device()
+    q = normal_bits(rng, 1, new, 2 * group, 128)
+    got = attend(cache, [before], [new], q)
+    with np.errstate(invalid="ignore"):
+        want, weighted, size = PO.attention(cache.pool, cache.table, [before], [0, new], O.bf16_bits_to_f64(q), SCALE)
+    finite = np.isfinite(want)
+    assert not finite[0, :, group:, :2].any() and finite[0, :, :group].all() and finite[0, :, :, 5:].all()
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and (got[np.isinf(want)] == want[np.isinf(want)]).all()
+    with np.errstate(invalid="ignore"):
+        assert (np.abs(got - want) <= attention_bound(want, weighted, size, group * new))[finite].all()
+
+
 @pytest.mark.parametrize("new", [[2, 40], [0, 0]])
 def test_tokens_past_max_new_are_left_out(new):
     rng = np.random.default_rng(8)
