@@ -29,6 +29,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kRowBytes = 2 * kHeadDim;      // of a bf16 row
 constexpr int kFp4RowBytes = kHeadDim / 2;   // the codes of an FP4 row; and 4 scale bytes
+constexpr float kLargestFp4Scale = 0x1p125f;  // of finite values: 6 * 2^125 is a bf16, 6 * 2^126 is not
 constexpr unsigned kFp4Bad = 255;            // scale byte of a group with a value that is not finite
 
 // Row number of slot 0 of a page of one head.
@@ -66,14 +67,18 @@ __device__ __forceinline__ unsigned fp4_pack8(u32x4 x, unsigned scale_byte) {
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, x3), s, 3);
   return scale_byte == kFp4Bad ? 0u : c;
 }
+// Codes 2i and 2i + 1 of eight.
+__device__ __forceinline__ unsigned fp4_unpack2(unsigned c, float s, int i) {
+  switch (i) {
+    case 0: return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+    case 1: return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+    case 2: return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+    default: return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
+  }
+}
 // Eight codes as bf16 values.  A group without a scale (255) is NaN: the conversion makes its values so.
 __device__ __forceinline__ u32x4 fp4_unpack8(unsigned c, float s) {
-  u32x4 x;
-  x[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
-  x[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
-  x[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
-  x[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
-  return x;
+  return u32x4{fp4_unpack2(c, s, 0), fp4_unpack2(c, s, 1), fp4_unpack2(c, s, 2), fp4_unpack2(c, s, 3)};
 }
 
 // The larger of the two magnitudes in a dword.

@@ -5,6 +5,7 @@
 
 #include "kernel_args.h"
 #include "paged.h"
+#include "wave_scan.h"
 
 namespace dapq {
 namespace {
@@ -17,8 +18,9 @@ struct PagedAttentionParams {
   int64_t q_stride_layer, q_stride_row, q_stride_head;
   float* parts;  // of the workspace
   int32_t batch, total_new, each_new, max_new, n_q_heads;
-  int32_t group, items, groups;  // query heads of a KV head; layers * Hkv; workgroups of the row kernel
-  float inv_group, c, cap;       // c: scale * log2(e), with a cap scale / softcap; cap: softcap * log2(e)
+  int32_t group, items, groups, least_share;  // query heads of a KV head; layers * Hkv; workgroups of the row kernel; fewest tiles of one
+  float inv_group, inv_items, inv_groups;
+  float c, cap;       // c: scale * log2(e), with a cap scale / softcap; cap: softcap * log2(e)
   float scale, softcap;
 };
 
@@ -103,6 +105,7 @@ constexpr int kRowWaves = 4;           // of a workgroup of the row kernel
 constexpr float kHeadroom = 4.0f;      // binades that a logit may lie above the reference of its column
 constexpr float kLowest = -3.4028234663852886e38f;  // where references start: finite, a logit of -inf then weighs 0
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr unsigned kNoPage = 0xffffffffu;
 
 // ---- how the row kernel shares out the rows ---------------------------------------------------------------------------
 // An item is one KV head of one sequence and layer, with all columns (new tokens x query heads of the KV head).  The tiles of all items, sequence by
@@ -118,6 +121,11 @@ struct Sequence {
 __device__ __forceinline__ int rows_seen(const PagedAttentionParams& p, int before, int t) {
   const int64_t most = (int64_t)p.pool.max_pages << p.pool.page_shift, n = (int64_t)before + t + 1;
   return (int)(n < 0 ? 0 : (n < most ? n : most));
+}
+// A value that the compiler can't trace: what is computed from it inside a loop is not kept in registers around the loop.
+__device__ __forceinline__ int opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ Sequence sequence(const PagedAttentionParams& p, int b) {
@@ -141,29 +149,31 @@ __device__ __forceinline__ Sequence uniform_sequence(const PagedAttentionParams&
 __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
-// The tiles of the sequences, 64 sequences at a time, one to a lane.
-template <typename F>
-__device__ __forceinline__ void walk_axis(const PagedAttentionParams& p, int lane, F each) {
-  int64_t before = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    int64_t n = b0 + lane < p.batch ? (int64_t)sequence(p, b0 + lane).tiles * p.items : 0;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t o = __shfl_up(n, d, 64);
-      if (lane >= d) n += o;
-    }
-    each(b0, before, n);  // n: tiles up to and with this lane's sequence, in this block of 64
-    before += uniform64(__shfl(n, 63, 64));
-  }
+// The tiles of 64 sequences from number b0 on, one sequence to a lane: its own, and the sum of an item's tiles up to and with it.
+struct Tiles {
+  Sequence own;
+  uint32_t upto;  // (64 x at most 2^25)
+};
+__device__ __forceinline__ Tiles tiles_of_64(const PagedAttentionParams& p, int b0, int lane) {
+  Tiles t;
+  t.own = {0, 0, 0, 0};
+  if (b0 + lane < p.batch) t.own = sequence(p, b0 + lane);
+  t.upto = wave_scan<OpAdd>((uint32_t)t.own.tiles);
+  return t;
 }
-__device__ __forceinline__ int64_t tiles_of_all(const PagedAttentionParams& p, int lane) {
-  int64_t total = 0;
-  walk_axis(p, lane, [&](int, int64_t before, int64_t n) { total = before + uniform64(__shfl(n, 63, 64)); });
-  return total;
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ __forceinline__ Sequence from_lane(const Sequence& s, int lane) {
+  return {__builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.tokens, lane), __builtin_amdgcn_readlane(s.before, lane),
+          __builtin_amdgcn_readlane(s.tiles, lane)};
+}
+// a / b of values that are the same in all lanes, inv = 1.0f / b.
+__device__ __forceinline__ int64_t divide(int64_t a, int b, float inv) {
+  return a < kQuotientMax ? __builtin_amdgcn_readfirstlane(quotient((int)a, inv)) : uniform64(a / b);
 }
 // A workgroup's length of the axis: at least a tile to a wave.
 __device__ __forceinline__ int64_t share_of(const PagedAttentionParams& p, int64_t total) {
-  const int64_t share = (total + p.groups - 1) / p.groups;
-  return share < kRowWaves ? kRowWaves : share;
+  const int64_t share = divide(total + p.groups - 1, p.groups, p.inv_groups);
+  return share < p.least_share ? p.least_share : share;
 }
 
 // A part of an item in the workspace: weighted sums, references and sums of weights of its columns.
@@ -172,8 +182,10 @@ struct Part {
   static constexpr int kFloats = COLS * (kHeadDim + 2);
 };
 
-// Whether one of the two bf16 of a dword is.
-__device__ __forceinline__ bool not_finite(unsigned x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+// The bits of those of the two bf16 of a dword that are infinite or no number.
+__device__ __forceinline__ unsigned infinite_bits(unsigned x) {
+  return ((x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
 
 // log2 of a weight before the reference is taken off: c * logit, or with a cap cap * log2(e) * tanh(logit * scale / cap).
 template <bool CAP>
@@ -193,13 +205,14 @@ __device__ __forceinline__ float capped(const PagedAttentionParams& p, float d) 
 //   output   D[column][channel] += weights (A) x V (B); a weight enters as two bf16 numbers, the leading 8 bits of its significand and the next 8.
 //            V is transposed in registers: a lane loads the same 8 channels of 8 rows.
 // BLOCKS: blocks of 16 columns; 0: up to 8 columns, whose leading and following parts take the two halves of one block.
-template <bool FP4, int BLOCKS, bool CAP>
-__global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAttentionParams p) {
+// SPLIT: a workgroup has its length of the axis; else an item (and nothing is to be joined).
+template <bool FP4, int BLOCKS, bool CAP, bool SPLIT>
+__global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_rows_kernel(PagedAttentionParams p) {
+  touch_args<sizeof(PagedAttentionParams)>();
   constexpr bool kHalf = BLOCKS == 0;
   constexpr int NB = kHalf ? 1 : BLOCKS, kCols = kHalf ? 8 : 16 * BLOCKS;
   constexpr int kWaveFloats = NB * 16 * (kHeadDim + 2);
   constexpr bool kQueriesInLds = NB == 2;  // (there are no registers for them)
-  constexpr bool kLate = NB == 2 && !FP4;  // the next keys are loaded where registers are left for them
   static_assert(!kQueriesInLds || kRowWaves == 4, "a wave brings in half a block");
   extern __shared__ float lds[];  // [waves]: weighted sums, references, sums of weights; queries
   bf16x8* queries = reinterpret_cast<bf16x8*>(lds + kRowWaves * kWaveFloats);
@@ -207,26 +220,39 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   float* mine = lds + wave * kWaveFloats;
   const int g = p.group;
+  // the columns of up to 8: the second half of a block has what the leading parts of the weights leave
+  const unsigned rest_mask = n >= 8 ? 0xffff0000u : 0u;
+  const float rest_factor = n >= 8 ? 1.0f + 0x1p-22f : 1.0f;
 
   // this workgroup's part of the axis, and the sequence it starts in
-  const int64_t share = share_of(p, tiles_of_all(p, lane));
-  const int64_t from = (int64_t)blockIdx.x * share;
-  int seq = p.batch;
-  int64_t seq_from = 0;
-  walk_axis(p, lane, [&](int b0, int64_t before, int64_t tiles) {
-    const uint64_t past = __ballot(before + tiles > from);
-    if (seq == p.batch && past != 0) {
-      const int at = __builtin_ctzll(past);
-      seq = b0 + at;
-      seq_from = before + (at > 0 ? uniform64(__shfl(tiles, at > 0 ? at - 1 : 0, 64)) : 0);
+  int seq, item, tile0;
+  int64_t left;
+  Sequence s;
+  if constexpr (SPLIT) {
+    Tiles t = tiles_of_64(p, 0, lane);
+    int64_t total = from_lane(t.upto, 63);
+    for (int b0 = 64; b0 < p.batch; b0 += 64) total += from_lane(tiles_of_64(p, b0, lane).upto, 63);
+    left = share_of(p, total * p.items);
+    int64_t at = (int64_t)blockIdx.x * left;  // (from the start of the 64 sequences)
+    for (seq = 0; at >= (int64_t)from_lane(t.upto, 63) * p.items;) {
+      at -= (int64_t)from_lane(t.upto, 63) * p.items;
+      seq += 64;
+      if (seq >= p.batch) return;
+      t = tiles_of_64(p, seq, lane);
     }
-  });
-  if (seq >= p.batch) return;
-  int64_t left = uniform64(share);
-  seq = uniform(seq);
-  Sequence s = uniform_sequence(p, seq);
-  int item = uniform((int)((from - seq_from) / s.tiles));  // layer * Hkv + head
-  int tile0 = uniform((int)((from - seq_from) - (int64_t)item * s.tiles));
+    const int l = __builtin_ctzll(__ballot(t.upto > (uint32_t)divide(at, p.items, p.inv_items)));
+    seq += l;
+    s = from_lane(t.own, l);
+    at -= (int64_t)(from_lane(t.upto, l) - s.tiles) * p.items;
+    item = (int)divide(at, s.tiles, 1.0f / (float)s.tiles);  // layer * Hkv + head
+    tile0 = (int)(at - (int64_t)item * s.tiles);
+  } else {
+    seq = (int)divide(blockIdx.x, p.items, p.inv_items);
+    item = blockIdx.x - seq * p.items;
+    s = uniform_sequence(p, seq);
+    tile0 = 0;
+    left = s.tiles;
+  }
 
   while (left > 0) {
     const int tile1 = uniform(s.tiles - tile0 < left ? s.tiles : tile0 + (int)left);
@@ -237,7 +263,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
     int vis[NB];
 #pragma unroll
     for (int t = 0; t < NB; ++t) {
-      int col = kHalf ? n & 7 : 16 * t + n;
+      int col = kHalf ? opaque(n) & 7 : 16 * t + opaque(n);
       col = col < cols ? col : cols - 1;
       const int token = quotient(col, p.inv_group), h = head * g + col - token * g;
       vis[t] = rows_seen(p, s.before, token);
@@ -251,69 +277,70 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
       }
     }
     if (kQueriesInLds) __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);  // (loads of queries behind those of the first tile would be waited for in every step)
     const int seen_by_all = rows_seen(p, s.before, 0), seen_by_last = rows_seen(p, s.before, s.tokens - 1);
 
     // pages of this wave's tiles, 64 tiles at a time, one to a lane
     const int32_t* table = p.pool.table + (int64_t)seq * p.pool.max_pages;
-    int page0 = -1, page1 = -1;
+    // as the number of 16 rows that the halves of a tile are (the rows of a pool over 16: below 2^32)
+    unsigned half0 = kNoPage, half1 = kNoPage;
     auto load_pages = [&](int k) {
-      int l = lane;
-      asm volatile("" : "+v"(l));
-      const int64_t tile = (int64_t)tile0 + wave + (int64_t)kRowWaves * (k + l);
-      page0 = page1 = -1;
-      if (tile < tile1) {
-        const int64_t e0 = tile * kTile >> p.pool.page_shift, e1 = (tile * kTile + 16) >> p.pool.page_shift;
-        page0 = e0 < p.pool.max_pages ? table[e0] : -1;
-        page1 = e1 < p.pool.max_pages ? table[e1] : -1;
-        if (page0 >= p.pool.n_pages) page0 = -1;
-        if (page1 >= p.pool.n_pages) page1 = -1;
-      }
+      const int64_t row = ((int64_t)tile0 + wave + (int64_t)kRowWaves * (k + opaque(lane))) * kTile;
+      const bool there = row < (int64_t)tile1 * kTile;
+      const int64_t last = p.pool.max_pages - 1, e0 = row >> p.pool.page_shift, e1 = (row + 16) >> p.pool.page_shift;
+      const int page0 = table[there ? (e0 < last ? e0 : last) : 0], page1 = table[there ? (e1 < last ? e1 : last) : 0];
+      auto sixteen = [&](int64_t e, int page, int64_t r) {
+        if (!there || e > last || page < 0 || page >= p.pool.n_pages) return kNoPage;
+        return (unsigned)((page_row(p.pool, layer, page, head) + (r & ((1 << p.pool.page_shift) - 1))) >> 4);
+      };
+      half0 = sixteen(e0, page0, row);
+      half1 = sixteen(e1, page1, row + 16);
     };
     struct Rows {
-      int64_t at[2];  // row numbers of the two halves of a tile (of page 0 where they are on no page)
+      unsigned at[2];
       bool ok[2];
     };
     auto rows_of = [&](int k) {
       if ((k & 63) == 0) load_pages(k);
-      Rows r;
-      const int64_t tile = (int64_t)tile0 + wave + (int64_t)kRowWaves * k;
-      const int pa = __builtin_amdgcn_readlane(page0, k & 63), pb = __builtin_amdgcn_readlane(page1, k & 63);
-      const int slot = (int)(tile * kTile) & ((1 << p.pool.page_shift) - 1), slot1 = (int)(tile * kTile + 16) & ((1 << p.pool.page_shift) - 1);
-      r.ok[0] = pa >= 0;
-      r.ok[1] = pb >= 0;
-      r.at[0] = uniform64(page_row(p.pool, layer, pa < 0 ? 0 : pa, head) + slot);
-      r.at[1] = uniform64(page_row(p.pool, layer, pb < 0 ? 0 : pb, head) + slot1);
-      return r;
+      const unsigned a = __builtin_amdgcn_readlane(half0, k & 63), b = __builtin_amdgcn_readlane(half1, k & 63);
+      return Rows{{a, b}, {a != kNoPage, b != kNoPage}};
     };
     // A tile in registers.  Keys: the operand (bf16), or a row's group of 32 channels to a lane.  Values: 8 channels of the rows
     // 16 * (e / 4) + 4 * kg + e % 4.
-    u32x4 kf[2][FP4 ? 1 : 4];
-    unsigned ks[2];
-    u32x4 vt[FP4 ? 1 : 8];
-    unsigned vc[8];
-    u32x4 vs[2];
-    // (through descriptors of 16 rows each: the address of a lane is an offset of 32 bits)
+    struct Buffer {
+      u32x4 kf[2][FP4 ? 1 : 4];
+      unsigned ks[2];
+      u32x4 vt[FP4 ? 1 : 8];
+      unsigned vc[8];
+      u32x4 vs[2];
+      Rows rows;
+    };
+    Buffer b;
+    // (through descriptors of 16 rows each: the address of a lane is an offset of 32 bits, and what is on no page is not read)
     const unsigned k_at = n * (FP4 ? kFp4RowBytes : kRowBytes) + kg * 16, v_at = 4 * kg * (FP4 ? kFp4RowBytes : kRowBytes) + n * (FP4 ? 4 : 16);
-    auto rows16 = [&](uint8_t* pool, int64_t at, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(pool + at * bytes, 0, 16 * bytes, 0x00020000); };
+    auto rows16 = [&](uint8_t* pool, const Rows& r, int hf, int bytes) {
+      return __builtin_amdgcn_make_buffer_rsrc(pool + (uint64_t)(r.ok[hf] ? r.at[hf] : 0) * (16 * bytes), 0, r.ok[hf] ? 16 * bytes : 0, 0x00020000);
+    };
     auto load_k = [&](const Rows& r) {
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        const auto src = rows16(p.pool.k, r.at[hf], FP4 ? kFp4RowBytes : kRowBytes);
+        const auto src = rows16(p.pool.k, r, hf, FP4 ? kFp4RowBytes : kRowBytes);
 #pragma unroll
-        for (int i = 0; i < (FP4 ? 1 : 4); ++i) kf[hf][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)k_at + i * 64, 0, 0));
-        if constexpr (FP4) ks[hf] = __builtin_amdgcn_raw_buffer_load_b8(rows16(p.pool.k_scales, r.at[hf], 4), n * 4 + kg, 0, 0);
+        for (int i = 0; i < (FP4 ? 1 : 4); ++i) b.kf[hf][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)k_at + i * 64, 0, 0));
+        if constexpr (FP4) b.ks[hf] = __builtin_amdgcn_raw_buffer_load_b8(rows16(p.pool.k_scales, r, hf, 4), n * 4 + kg, 0, 0);
       }
     };
     auto load_v = [&](const Rows& r) {
+      b.rows = r;
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        const auto src = rows16(p.pool.v, r.at[hf], FP4 ? kFp4RowBytes : kRowBytes);
+        const auto src = rows16(p.pool.v, r, hf, FP4 ? kFp4RowBytes : kRowBytes);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if constexpr (FP4) vc[4 * hf + e] = __builtin_amdgcn_raw_buffer_load_b32(src, (int)v_at + e * kFp4RowBytes, 0, 0);
-          else vt[4 * hf + e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)v_at + e * kRowBytes, 0, 0));
+          if constexpr (FP4) b.vc[4 * hf + e] = __builtin_amdgcn_raw_buffer_load_b32(src, (int)v_at + e * kFp4RowBytes, 0, 0);
+          else b.vt[4 * hf + e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)v_at + e * kRowBytes, 0, 0));
         }
-        if constexpr (FP4) vs[hf] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows16(p.pool.v_scales, r.at[hf], 4), 16 * kg, 0, 0));
+        if constexpr (FP4) b.vs[hf] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows16(p.pool.v_scales, r, hf, 4), 16 * kg, 0, 0));
       }
     };
 
@@ -330,15 +357,10 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
     }
 
     bool apart = false;  // whether there are such values
-    Rows now = {};
-    if (tile0 + wave < tile1) {
-      now = rows_of(0);
-      load_k(now);
-      load_v(now);
-    }
-    for (int k = 0; tile0 + wave + kRowWaves * k < tile1; ++k) {
+    // Tile number k of this wave, and the loads of the next one as the registers of this one are spent: always, or the waits could not count them.
+    auto step = [&](int k) {
       const int row0 = (tile0 + wave + kRowWaves * k) * kTile;
-      const bool more = tile0 + wave + kRowWaves * (k + 1) < tile1;
+      const Rows now = b.rows;
       const bool partial = row0 + kTile > seen_by_all || !now.ok[0] || !now.ok[1];
       float xs[NB][8];
 #pragma unroll
@@ -349,8 +371,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           u32x4 a;
-          if constexpr (FP4) a = fp4_unpack8(kf[hf][0][i], fp4_scale(ks[hf]));
-          else a = kf[hf][i];
+          if constexpr (FP4) a = fp4_unpack8(b.kf[hf][0][i], fp4_scale(b.ks[hf]));
+          else a = b.kf[hf][i];
 #pragma unroll
           for (int t = 0; t < NB; ++t)
             d[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), kQueriesInLds ? queries[(t * 4 + i) * 64 + lane] : qf[kQueriesInLds ? 0 : t][i], d[t], 0, 0, 0);
@@ -360,11 +382,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
 #pragma unroll
           for (int v = 0; v < 4; ++v) xs[t][4 * hf + v] = capped<CAP>(p, d[t][v]);
       }
-      Rows next = now;
-      if (more) {
-        next = rows_of(k + 1);
-        if (!kLate) load_k(next);
-      }
+      const Rows next = rows_of(k + 1);
+      load_k(next);
       __builtin_amdgcn_sched_barrier(0);
       u32x4 hi[NB], lo[NB];  // the weights as A operand
 #pragma unroll
@@ -404,8 +423,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
           const float y = __builtin_amdgcn_exp2f(CAP ? x[e] - ref[t] : fmaf(x[e], p.c, -ref[t]));
           sum[t] += y;
           // what the leading part leaves, and 2^-22 of the weight, which keeps it from 0 where a value is infinite
-          const float rest = fmaf(y, 1.0f + 0x1p-22f, -__uint_as_float(__float_as_uint(y) & 0xffff0000u));
-          w[e] = __float_as_uint(kHalf && n >= 8 ? rest : y);
+          const float rest = fmaf(y, kHalf ? rest_factor : 1.0f + 0x1p-22f, -__uint_as_float(__float_as_uint(y) & (kHalf ? rest_mask : 0xffff0000u)));
+          w[e] = __float_as_uint(kHalf ? rest : y);
           w2[e] = __float_as_uint(rest);
         }
 #pragma unroll
@@ -414,64 +433,91 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
           lo[t][e] = __builtin_amdgcn_perm(w2[2 * e + 1], w2[2 * e], 0x07060302u);
         }
       }
-      u32x4 vr[8];
+      float vscale[8];  // FP4: of the rows, for this lane's channels
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (FP4) vr[e] = fp4_unpack8(vc[e], fp4_scale((vs[e >> 2][e & 3] >> (8 * (n >> 2))) & 255u));
-        else vr[e] = vt[e];
-      }
+      for (int e = 0; e < 8; ++e) vscale[e] = FP4 ? fp4_scale((b.vs[e >> 2][e & 3] >> (8 * (n >> 2))) & 255u) : 0.0f;
       if (partial) {
         // Rows that no column sees may hold anything, and 0 times it must be 0.  A value that is infinite or no number, in a row that some columns
-        // see and others don't, is added to the former by itself (in LDS: sums of such values are what they are in any order).
+        // see and others don't, is added to the former by itself, in LDS.
         bool odd = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int row = row0 + 16 * (e >> 2) + 4 * kg + (e & 3);
-          if (row >= seen_by_last || !now.ok[e >> 2]) vr[e] = u32x4{0, 0, 0, 0};
-          if (row >= seen_by_all) odd |= not_finite(vr[e][0]) || not_finite(vr[e][1]) || not_finite(vr[e][2]) || not_finite(vr[e][3]);
-        }
-        if (__any(odd)) {
-          int n8 = 8 * n, row4 = row0 + 4 * kg;
-          asm volatile("" : "+v"(n8), "+v"(row4));  // (nothing of this is to be kept in registers outside)
-          if (!apart) {
-            for (int i = lane; i < kCols * kHeadDim; i += 64) mine[i] = 0.0f;
-            apart = true;
-          }
+          const bool none = row >= seen_by_last || !now.ok[e >> 2];
+          if constexpr (FP4) {
+            const bool bad = vscale[e] > kLargestFp4Scale || vscale[e] != vscale[e];
+            odd |= bad && !none && row >= seen_by_all;
+            if (none || (bad && row >= seen_by_all)) {
+              b.vc[e] = 0;
+              vscale[e] = 1.0f;
+            }
+          } else {
+            if (none) b.vt[e] = u32x4{0, 0, 0, 0};
+            if (row >= seen_by_all) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int row = row4 + 16 * (e >> 2) + (e & 3);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const unsigned all = vr[e][i];
-              const unsigned bad = row >= seen_by_all ? all & (((all & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((all & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u)) : 0u;
-              vr[e][i] = all & ~bad;
-              if (bad == 0) continue;
-#pragma unroll 1
-              for (int col = 0; col < cols; ++col) {
-                if (row >= rows_seen(p, s.before, quotient(col, p.inv_group))) continue;
-                atomicAdd(mine + col * kHeadDim + n8 + 2 * i, __uint_as_float(bad << 16));
-                atomicAdd(mine + col * kHeadDim + n8 + 2 * i + 1, __uint_as_float(bad & 0xffff0000u));
+              for (int i = 0; i < 4; ++i) {
+                const unsigned bad = infinite_bits(b.vt[e][i]);
+                odd |= bad != 0;
+                b.vt[e][i] &= ~bad;
               }
             }
           }
         }
-      }
-      if (kLate && more) load_k(next);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {  // channels 8 * n + j
-        u32x4 vb;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) vb[e] = __builtin_amdgcn_perm(vr[2 * e + 1][j >> 1], vr[2 * e][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
-#pragma unroll
-        for (int t = 0; t < NB; ++t) {
-          acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi[t]), __builtin_bit_cast(bf16x8, vb), acc[t][j], 0, 0, 0);
-          if constexpr (!kHalf)
-            acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo[t]), __builtin_bit_cast(bf16x8, vb), acc[t][j], 0, 0, 0);
+        if (__any(odd)) {
+          if (!apart) {
+            for (int i = lane; i < kCols * kHeadDim; i += 64) mine[i] = 0.0f;
+            apart = true;
+          }
+#pragma unroll 1
+          for (int row = row0 > seen_by_all ? row0 : seen_by_all; row < row0 + kTile && row < seen_by_last; ++row) {  // once more, two channels to a lane
+            const int i = row - row0;
+            if (!(i < 16 ? now.ok[0] : now.ok[1])) continue;
+            const int64_t at = (int64_t)(i < 16 ? now.at[0] : now.at[1]) * 16 + (i & 15);
+            unsigned u;
+            if constexpr (FP4) u = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((unsigned)p.pool.v[at * kFp4RowBytes + lane], fp4_scale(p.pool.v_scales[at * 4 + (lane >> 4)]), 0));
+            else u = *reinterpret_cast<const unsigned*>(p.pool.v + at * kRowBytes + lane * 4);
+            u &= infinite_bits(u);
+            if (!__any(u != 0)) continue;
+#pragma unroll 1
+            for (int col = 0; col < cols; ++col) {
+              if (row >= rows_seen(p, s.before, quotient(col, p.inv_group))) continue;
+              mine[col * kHeadDim + 2 * lane] += __uint_as_float(u << 16);
+              mine[col * kHeadDim + 2 * lane + 1] += __uint_as_float(u & 0xffff0000u);
+            }
+          }
         }
       }
-      if (more) load_v(next);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // channels 8 * n + 2 * i and the one behind it
+        unsigned x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if constexpr (FP4) x[e] = fp4_unpack2(b.vc[e], vscale[e], i);
+          else x[e] = b.vt[e][i];
+        }
+#pragma unroll
+        for (int j = 2 * i; j < 2 * i + 2; ++j) {
+          u32x4 vb;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vb[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], (j & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int t = 0; t < NB; ++t) {
+            acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi[t]), __builtin_bit_cast(bf16x8, vb), acc[t][j], 0, 0, 0);
+            if constexpr (!kHalf)
+              acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo[t]), __builtin_bit_cast(bf16x8, vb), acc[t][j], 0, 0, 0);
+          }
+        }
+      }
+      load_v(next);
       __builtin_amdgcn_sched_barrier(0);
-      now = next;
+    };
+    if (tile0 + wave < tile1) {
+      const int tiles = (tile1 - tile0 - wave + kRowWaves - 1) / kRowWaves;
+      const Rows first = rows_of(0);
+      load_k(first);
+      load_v(first);
+      __builtin_amdgcn_sched_barrier(0);
+      for (int k = 0; k < tiles; ++k) step(k);
     }
 
     // what the waves have, in LDS
@@ -490,23 +536,22 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
       w += __shfl_xor(w, 32, 64);
       const uint64_t any = __ballot(seen[t]);
       const bool column = (any >> n | any >> (n + 16) | any >> (n + 32) | any >> (n + 48)) & 1;
+      const int n8 = opaque(8 * n);
       if (kg == 0) {
         mine[NB * 16 * kHeadDim + 16 * t + n] = column ? ref[t] : -INFINITY;  // (no row was seen)
         mine[NB * 16 * (kHeadDim + 1) + 16 * t + n] = w;
       }
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        f32x4* dst = reinterpret_cast<f32x4*>(mine + (16 * t + 4 * kg + v) * kHeadDim + 8 * n);
+        f32x4* dst = reinterpret_cast<f32x4*>(mine + (16 * t + 4 * kg + v) * kHeadDim + n8);
         dst[0] = f32x4{acc[t][0][v], acc[t][1][v], acc[t][2][v], acc[t][3][v]};
         dst[1] = f32x4{acc[t][4][v], acc[t][5][v], acc[t][6][v], acc[t][7][v]};
       }
     }
     __syncthreads();
-    const bool whole = tile0 == 0 && tile1 == s.tiles;
+    const bool whole = !SPLIT || (tile0 == 0 && tile1 == s.tiles);
     float* part = p.parts + ((int64_t)blockIdx.x * 2 + (tile0 == 0 ? 1 : 0)) * Part<kCols>::kFloats;
-    int e0 = tid;
-    asm volatile("" : "+v"(e0));  // (as above: no registers for this during the loop)
-    for (int e = e0; e < cols * (kHeadDim / 2); e += 64 * kRowWaves) {
+    for (int e = opaque(tid); e < cols * (kHeadDim / 2); e += 64 * kRowWaves) {
       const int col = e / (kHeadDim / 2), c = 2 * (e % (kHeadDim / 2));
       float m = -INFINITY;
 #pragma unroll
@@ -540,6 +585,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
         }
       }
     }
+    if (!SPLIT) return;
     left = uniform64(left - (tile1 - tile0));
     tile0 = 0;
     if (++item == p.items) {
@@ -553,71 +599,129 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedAtte
   }
 }
 
-// The items that several workgroups share: their parts, in order.  A workgroup per item.
+// The items that several workgroups share: a workgroup per item and column, its waves take the parts in turn and meet in LDS.
+constexpr int kJoinWaves = 8;
 template <int COLS>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttentionParams p) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int seq = blockIdx.x / p.items, item = blockIdx.x - seq * p.items;
-  const Sequence s = sequence(p, seq);
-  if (s.tiles == 0) return;
-  int64_t total = 0, from = 0;
-  walk_axis(p, lane, [&](int b0, int64_t before, int64_t n) {
-    total = before + uniform64(__shfl(n, 63, 64));
-    if (seq >= b0 && seq < b0 + 64) from = before + (seq > b0 ? uniform64(__shfl(n, seq > b0 ? seq - b0 - 1 : 0, 64)) : 0);
-  });
-  const int64_t share = share_of(p, total);
-  from += (int64_t)item * s.tiles;
-  const int64_t first = from / share, last = (from + s.tiles - 1) / share;
-  if (first == last) return;
-  const int layer = item / p.pool.n_kv_heads, head = item - layer * p.pool.n_kv_heads;
-  for (int e = tid; e < s.tokens * p.group * (kHeadDim / 2); e += 256) {
-    const int col = e / (kHeadDim / 2), c = 2 * (e % (kHeadDim / 2));
-    auto part = [&](int64_t w) { return p.parts + (w * 2 + (w == first ? 1 : 0)) * Part<COLS>::kFloats; };
-    float m = -INFINITY;
-    for (int64_t w = first; w <= last; ++w) m = fmaxf(m, part(w)[COLS * kHeadDim + col]);
-    f32x2 o = {0.0f, 0.0f};
-    float sum = 0.0f;
-    for (int64_t w = first; w <= last; ++w) {
-      const float r = part(w)[COLS * kHeadDim + col];
-      if (r == -INFINITY) continue;
-      const float f = __builtin_amdgcn_exp2f(r - m);
-      const f32x2 x = *reinterpret_cast<const f32x2*>(part(w) + col * kHeadDim + c);
-      o[0] = fmaf(f, x[0], o[0]);
-      o[1] = fmaf(f, x[1], o[1]);
-      sum = fmaf(f, part(w)[COLS * (kHeadDim + 1) + col], sum);
+__global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttentionParams p) {
+  __shared__ float wave_sums[kJoinWaves][kHeadDim + 2];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int seq = (int)divide(blockIdx.x, p.items, p.inv_items), item = blockIdx.x - seq * p.items, col = blockIdx.y;
+  Tiles t = tiles_of_64(p, 0, lane);
+  int64_t total = from_lane(t.upto, 63), from = 0;  // (tiles of an item)
+  Sequence s = from_lane(t.own, seq & 63);
+  if (seq < 64) from = from_lane(t.upto, seq);
+  for (int b0 = 64; b0 < p.batch; b0 += 64) {
+    t = tiles_of_64(p, b0, lane);
+    if (seq >= b0 && seq < b0 + 64) {
+      s = from_lane(t.own, seq & 63);
+      from = total + from_lane(t.upto, seq & 63);
     }
-    const int token = quotient(col, p.inv_group), h = head * p.group + col - token * p.group;
-    bf16x2 result;
-    result[0] = (__bf16)(m == -INFINITY ? 0.0f : o[0] / sum);
-    result[1] = (__bf16)(m == -INFINITY ? 0.0f : o[1] / sum);
-    *reinterpret_cast<bf16x2*>(p.out + (((int64_t)layer * p.total_new + s.first + token) * p.n_q_heads + h) * kHeadDim + c) = result;
+    total += from_lane(t.upto, 63);
   }
+  if (s.tiles == 0 || col >= s.tokens * p.group) return;
+  const int64_t share = share_of(p, total * p.items);
+  from = (from - s.tiles) * p.items + (int64_t)item * s.tiles;
+  const float inv = 1.0f / (float)share;
+  const int first = (int)(share < kQuotientMax ? divide(from, (int)share, inv) : from / share);
+  const int parts = (int)(share < kQuotientMax ? divide(from + s.tiles - 1, (int)share, inv) : (from + s.tiles - 1) / share) - first + 1;
+  if (parts == 1) return;
+  auto part = [&](int i) { return p.parts + ((int64_t)(first + i) * 2 + (i == 0 ? 1 : 0)) * Part<COLS>::kFloats; };
+  float m = -INFINITY, sum = 0.0f;
+  f32x2 o = {0.0f, 0.0f};
+  for (int i0 = wave; i0 < parts; i0 += kJoinWaves * 64) {  // 64 parts of this wave, one to a lane
+    const int mine = i0 + kJoinWaves * lane, n = (parts - i0 + kJoinWaves - 1) / kJoinWaves < 64 ? (parts - i0 + kJoinWaves - 1) / kJoinWaves : 64;
+    const float r = mine < parts ? part(mine)[COLS * kHeadDim + col] : -INFINITY;
+    float w = mine < parts ? part(mine)[COLS * (kHeadDim + 1) + col] : 0.0f;
+    float top = r;
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float moved = fmaxf(m, top);
+    if (moved == -INFINITY) continue;
+    const float f = __builtin_amdgcn_exp2f(r - moved), before = __builtin_amdgcn_exp2f(m - moved);  // (parts without a row: 0)
+    w = f == 0.0f && r == -INFINITY ? 0.0f : w * f;
+    for (int d = 32; d > 0; d >>= 1) w += __shfl_xor(w, d, 64);
+    sum = m == -INFINITY ? w : fmaf(sum, before, w);
+    if (m != -INFINITY) o *= before;
+    m = moved;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const f32x2 x = *reinterpret_cast<const f32x2*>(part(i0 + kJoinWaves * i) + col * kHeadDim + 2 * lane);
+      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+      if (__builtin_amdgcn_readlane(__float_as_uint(r), i) == 0xff800000u) continue;
+      o[0] = fmaf(fi, x[0], o[0]);
+      o[1] = fmaf(fi, x[1], o[1]);
+    }
+  }
+  *reinterpret_cast<f32x2*>(&wave_sums[wave][2 * lane]) = o;
+  if (lane == 0) {
+    wave_sums[wave][kHeadDim] = m;
+    wave_sums[wave][kHeadDim + 1] = sum;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  const int waves = parts < kJoinWaves ? parts : kJoinWaves;
+  m = -INFINITY;
+  for (int w = 0; w < waves; ++w) m = fmaxf(m, wave_sums[w][kHeadDim]);
+  o = f32x2{0.0f, 0.0f};
+  sum = 0.0f;
+  for (int w = 0; w < waves; ++w) {  // (in order)
+    if (wave_sums[w][kHeadDim] == -INFINITY) continue;
+    const float f = __builtin_amdgcn_exp2f(wave_sums[w][kHeadDim] - m);
+    o[0] = fmaf(f, wave_sums[w][2 * lane], o[0]);
+    o[1] = fmaf(f, wave_sums[w][2 * lane + 1], o[1]);
+    sum = fmaf(f, wave_sums[w][kHeadDim + 1], sum);
+  }
+  const int layer = item / p.pool.n_kv_heads, head = item - layer * p.pool.n_kv_heads;
+  const int token = quotient(col, p.inv_group), h = head * p.group + col - token * p.group;
+  bf16x2 result;
+  result[0] = (__bf16)(m == -INFINITY ? 0.0f : o[0] / sum);
+  result[1] = (__bf16)(m == -INFINITY ? 0.0f : o[1] / sum);
+  *reinterpret_cast<bf16x2*>(p.out + (((int64_t)layer * p.total_new + s.first + token) * p.n_q_heads + h) * kHeadDim + 2 * lane) = result;
 }
 
-// Workgroups of the row kernel: as many as the chip holds at a time, and no more than there is work for.
-int row_groups(const dapq_pages* p) {
-  const int64_t most = (((int64_t)p->max_pages * p->page_rows + kTile - 1) / kTile) * p->n_layers * p->batch * p->n_kv_heads;
-  const int64_t groups = (most + kRowWaves - 1) / kRowWaves;
-  return (int)(groups < 512 ? groups : 512);
-}
 constexpr int kMostRowCols = 32;
 int row_cols(int64_t cols) { return cols <= 8 ? 8 : (cols <= 16 ? 16 : 32); }
 
-template <bool FP4, int BLOCKS>
+// How a call of up to 32 columns is run: a function of the descriptors alone, which the workspace follows.
+struct RowPlan {
+  bool split;
+  int groups;
+};
+RowPlan row_plan(const dapq_pages* p, int cols) {
+  const int64_t tiles = ((int64_t)p->max_pages * p->page_rows + kTile - 1) / kTile;  // of an item, at most
+  const int64_t items = (int64_t)p->n_layers * p->batch * p->n_kv_heads;
+  RowPlan plan;
+  plan.split = items < 256 && tiles > 40;
+  const int64_t groups = (tiles * items + kRowWaves - 1) / kRowWaves, chip = cols == 32 ? 512 : 768;
+  plan.groups = (int)(groups < chip ? groups : chip);
+  return plan;
+}
+
+template <bool FP4, int BLOCKS, bool SPLIT>
 int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, hipStream_t stream) {
   constexpr int kCols = BLOCKS == 0 ? 8 : 16 * BLOCKS, kBytes = kRowWaves * (BLOCKS == 0 ? 1 : BLOCKS) * 16 * (kHeadDim + 2) * 4 + (BLOCKS == 2 ? 8192 : 0);
-  auto kernel = p.cap > 0.0f ? paged_rows_kernel<FP4, BLOCKS, true> : paged_rows_kernel<FP4, BLOCKS, false>;
+  auto kernel = p.cap > 0.0f ? paged_rows_kernel<FP4, BLOCKS, true, SPLIT> : paged_rows_kernel<FP4, BLOCKS, false, SPLIT>;
   const int rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), kBytes);
   if (rc != DAPQ_OK) return rc;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)p.groups), dim3(64 * kRowWaves), kBytes, stream, p);
+  const unsigned items = (unsigned)(pages->batch * p.items);  // (below 2^24)
+  hipLaunchKernelGGL(kernel, dim3(SPLIT ? (unsigned)p.groups : items), dim3(64 * kRowWaves), kBytes, stream, p);
   DAPQ_HIP_LAUNCH_CHECK("paged_rows_kernel");
-  hipLaunchKernelGGL((paged_join_kernel<kCols>), dim3((unsigned)((int64_t)pages->batch * p.items)), dim3(256), 0, stream, p);
-  DAPQ_HIP_LAUNCH_CHECK("paged_join_kernel");
+  if (SPLIT) {
+    hipLaunchKernelGGL((paged_join_kernel<kCols>), dim3(items, (unsigned)(p.max_new * p.group)), dim3(64 * kJoinWaves), 0, stream, p);
+    DAPQ_HIP_LAUNCH_CHECK("paged_join_kernel");
+  }
   return DAPQ_OK;
 }
-template <bool FP4>
+template <bool FP4, bool SPLIT>
 int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, int cols, hipStream_t stream) {
-  return cols == 8 ? launch_rows<FP4, 0>(pages, p, stream) : (cols == 16 ? launch_rows<FP4, 1>(pages, p, stream) : launch_rows<FP4, 2>(pages, p, stream));
+  return cols == 8 ? launch_rows<FP4, 0, SPLIT>(pages, p, stream) : (cols == 16 ? launch_rows<FP4, 1, SPLIT>(pages, p, stream) : launch_rows<FP4, 2, SPLIT>(pages, p, stream));
+}
+int launch_rows(const dapq_pages* pages, PagedAttentionParams p, int cols, hipStream_t stream) {
+  const RowPlan plan = row_plan(pages, cols);
+  p.groups = plan.groups;
+  p.inv_groups = 1.0f / (float)plan.groups;
+  p.least_share = kRowWaves;
+  if (pages->format == DAPQ_PAGES_FP4) return plan.split ? launch_rows<true, true>(pages, p, cols, stream) : launch_rows<true, false>(pages, p, cols, stream);
+  return plan.split ? launch_rows<false, true>(pages, p, cols, stream) : launch_rows<false, false>(pages, p, cols, stream);
 }
 
 int check_attention(const dapq_pages* pages, const dapq_step* step) {
@@ -642,7 +746,7 @@ extern "C" DAPQ_API size_t dapq_paged_attention_workspace_bytes(const dapq_pages
   if (check_attention(pages, step) != DAPQ_OK) return 0;
   const int64_t cols = (int64_t)step->max_new * (step->n_q_heads / pages->n_kv_heads);
   if (cols > kMostRowCols) return 256;
-  return align_up((size_t)row_groups(pages) * 2 * row_cols(cols) * (kHeadDim + 2) * sizeof(float), 256);
+  return align_up((size_t)row_plan(pages, row_cols(cols)).groups * 2 * row_cols(cols) * (kHeadDim + 2) * sizeof(float), 256);
 }
 
 extern "C" DAPQ_API int dapq_paged_attention(const dapq_pages* pages, const dapq_step* step, const void* q, void* out, void* workspace,
@@ -674,14 +778,12 @@ extern "C" DAPQ_API int dapq_paged_attention(const dapq_pages* pages, const dapq
   p.parts = static_cast<float*>(workspace);
   p.group = step->n_q_heads / pages->n_kv_heads;
   p.items = pages->n_layers * pages->n_kv_heads;
-  p.groups = row_groups(pages);
   p.inv_group = 1.0f / (float)p.group;
+  p.inv_items = 1.0f / (float)p.items;
   p.cap = step->softcap * kLog2e;
   p.c = step->softcap > 0.0f ? step->scale / step->softcap : step->scale * kLog2e;
   const int64_t cols = (int64_t)step->max_new * p.group;
-  if (cols <= kMostRowCols)
-    return pages->format == DAPQ_PAGES_FP4 ? launch_rows<true>(pages, p, row_cols(cols), static_cast<hipStream_t>(stream))
-                                           : launch_rows<false>(pages, p, row_cols(cols), static_cast<hipStream_t>(stream));
+  if (cols <= kMostRowCols) return launch_rows(pages, p, row_cols(cols), static_cast<hipStream_t>(stream));
   hipLaunchKernelGGL(pages->format == DAPQ_PAGES_FP4 ? paged_attention_kernel<true> : paged_attention_kernel<false>,
                      dim3((unsigned)step->total_new, (unsigned)step->n_q_heads, (unsigned)pages->n_layers), dim3(64), 0,
                      static_cast<hipStream_t>(stream), p);
