@@ -1,110 +1,12 @@
 // Attention of a step's tokens over a cache in pages.
-#include <math.h>
-
-#include <type_traits>
-
-#include "kernel_args.h"
-#include "paged.h"
+#include "paged_attention.h"
 #include "wave_scan.h"
 
 namespace dapq {
 namespace {
 
-struct PagedAttentionParams {
-  PagePool pool;
-  const uint16_t* q;
-  uint16_t* out;
-  const int32_t *cu_new, *lengths;
-  int64_t q_stride_layer, q_stride_row, q_stride_head;
-  float* parts;  // of the workspace
-  int32_t batch, total_new, each_new, max_new, n_q_heads;
-  int32_t group, items, groups, least_share;  // query heads of a KV head; layers * Hkv; workgroups of the row kernel; fewest tiles of one
-  float inv_group, inv_items, inv_groups;
-  float c, cap;       // c: scale * log2(e), with a cap scale / softcap; cap: softcap * log2(e)
-  float scale, softcap;
-};
-
-// A wave to a token and query head: the logits of 64 rows at a time, one to a lane, then their values, two channels to a lane.
-template <bool FP4>
-__global__ __launch_bounds__(64) void paged_attention_kernel(PagedAttentionParams p) {
-  __shared__ float q[kHeadDim];
-  const int lane = threadIdx.x, r = blockIdx.x, h = blockIdx.y, layer = blockIdx.z;
-  const int kv = h / (p.n_q_heads / p.pool.n_kv_heads);
-  int seq = 0, start = 0;
-  if (p.cu_new == nullptr) {
-    seq = r / p.each_new;
-    start = seq * p.each_new;
-  } else {
-    while (seq < p.batch && p.cu_new[seq + 1] <= r) ++seq;
-    if (seq >= p.batch) return;
-    start = p.cu_new[seq];
-  }
-  if (r - start >= p.max_new) return;
-  const int64_t most = (int64_t)p.pool.max_pages << p.pool.page_shift;
-  const int64_t seen = (int64_t)p.lengths[seq] + (r - start) + 1;
-  const int visible = (int)(seen < most ? seen : most);
-  const uint16_t* src = p.q + layer * p.q_stride_layer + (int64_t)r * p.q_stride_row + h * p.q_stride_head;
-  q[lane] = __uint_as_float((unsigned)src[lane] << 16);
-  q[lane + 64] = __uint_as_float((unsigned)src[lane + 64] << 16);
-  __syncthreads();
-  auto value = [&](const uint8_t* rows, const uint8_t* scales, int64_t row, int c8) {
-    if constexpr (FP4) return fp4_unpack8(*reinterpret_cast<const unsigned*>(rows + row * kFp4RowBytes + c8 * 4), fp4_scale(scales[row * 4 + (c8 >> 2)]));
-    else return *reinterpret_cast<const u32x4*>(rows + row * kRowBytes + c8 * 16);
-  };
-  float m = -INFINITY, sum = 0.0f, o[2] = {0.0f, 0.0f};
-  for (int i0 = 0; i0 < visible; i0 += 64) {
-    const int64_t row = i0 + lane < visible ? find_row(p.pool, layer, seq, kv, i0 + lane) : -1;
-    float x = -INFINITY;
-    if (row >= 0) {
-      x = 0.0f;
-      for (int c8 = 0; c8 < 16; ++c8) {
-        const u32x4 k = value(p.pool.k, p.pool.k_scales, row, c8);
-        for (int i = 0; i < 4; ++i) {
-          x = fmaf(q[8 * c8 + 2 * i], __uint_as_float(k[i] << 16), x);
-          x = fmaf(q[8 * c8 + 2 * i + 1], __uint_as_float(k[i] & 0xffff0000u), x);
-        }
-      }
-      x *= p.scale;
-      if (p.softcap > 0.0f) x = p.softcap * tanhf(x / p.softcap);
-    }
-    float top = x;
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    if (__ballot(row >= 0) == 0) continue;
-    const float moved = fmaxf(fmaxf(m, top), -3.4028234663852886e38f);
-    const float f = expf(m - moved);
-    m = moved;
-    const float w = row >= 0 ? expf(x - m) : 0.0f;
-    float s = w;
-    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d, 64);
-    sum = sum * f + s;
-    o[0] *= f;
-    o[1] *= f;
-    for (int j = 0; j < 64; ++j) {
-      const int64_t rj = __shfl(row, j, 64);
-      const float wj = __shfl(w, j, 64);
-      if (rj < 0) continue;
-      const u32x4 v = value(p.pool.v, p.pool.v_scales, rj, lane >> 2);
-      const unsigned u = v[lane & 3];
-      o[0] = fmaf(wj, __uint_as_float(u << 16), o[0]);
-      o[1] = fmaf(wj, __uint_as_float(u & 0xffff0000u), o[1]);
-    }
-  }
-  const bool none = m == -INFINITY;  // no visible row is on a page
-  bf16x2 result;
-  result[0] = (__bf16)(none ? 0.0f : o[0] / sum);
-  result[1] = (__bf16)(none ? 0.0f : o[1] / sum);
-  *reinterpret_cast<bf16x2*>(p.out + (((int64_t)layer * p.total_new + r) * p.n_q_heads + h) * kHeadDim + 2 * lane) = result;
-}
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-constexpr int kTile = 32;              // cache rows that a wave takes at a time
-constexpr int kRowWaves = 4;           // of a workgroup of the row kernel
-constexpr float kHeadroom = 4.0f;      // binades that a logit may lie above the reference of its column
-constexpr float kLowest = -3.4028234663852886e38f;  // where references start: finite, a logit of -inf then weighs 0
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kTile = 32;     // cache rows that a wave takes at a time
+constexpr int kRowWaves = 4;  // of a workgroup
 constexpr unsigned kNoPage = 0xffffffffu;
 
 // ---- how the row kernel shares out the rows ---------------------------------------------------------------------------
@@ -117,17 +19,6 @@ struct Sequence {
   int tiles;          // of an item; 0 if it has no new tokens
 };
 
-// The rows that token t sees.
-__device__ __forceinline__ int rows_seen(const PagedAttentionParams& p, int before, int t) {
-  const int64_t most = (int64_t)p.pool.max_pages << p.pool.page_shift, n = (int64_t)before + t + 1;
-  return (int)(n < 0 ? 0 : (n < most ? n : most));
-}
-// A value that the compiler can't trace: what is computed from it inside a loop is not kept in registers around the loop.
-__device__ __forceinline__ int opaque(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ Sequence sequence(const PagedAttentionParams& p, int b) {
   Sequence s;
   s.first = p.cu_new == nullptr ? b * p.each_new : p.cu_new[b];
@@ -145,9 +36,6 @@ __device__ __forceinline__ Sequence sequence(const PagedAttentionParams& p, int 
 __device__ __forceinline__ Sequence uniform_sequence(const PagedAttentionParams& p, int b) {
   Sequence s = sequence(p, b);
   return {uniform(s.first), uniform(s.tokens), uniform(s.before), uniform(s.tiles)};
-}
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 // The tiles of 64 sequences from number b0 on, one sequence to a lane: its own, and the sum of an item's tiles up to and with it.
 struct Tiles {
@@ -181,23 +69,6 @@ template <int COLS>
 struct Part {
   static constexpr int kFloats = COLS * (kHeadDim + 2);
 };
-
-// The bits of those of the two bf16 of a dword that are infinite or no number.
-__device__ __forceinline__ unsigned infinite_bits(unsigned x) {
-  return ((x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-}
-
-// log2 of a weight before the reference is taken off: c * logit, or with a cap cap * log2(e) * tanh(logit * scale / cap).
-template <bool CAP>
-__device__ __forceinline__ float capped(const PagedAttentionParams& p, float d) {
-  if constexpr (!CAP) return d;  // (times p.c where it is used)
-  // tanh(z) = 1 - 2 / (1 + exp(2 z)) loses what z is smaller than 1 by: below 1/4 the series, whose first term left out is below 2^-22 z
-  const float z = d * p.c;
-  const float big = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * (2.0f * kLog2e))), 1.0f);
-  const float u = z * z;
-  const float small = z * fmaf(u, fmaf(u, fmaf(u, fmaf(u, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-  return p.cap * (fabsf(z) < 0.25f ? small : big);
-}
 
 // One wave per 32 rows at a time, the waves of a workgroup in turn over a part of an item; both products on v_mfma_f32_16x16x32_bf16.
 //   logits   D[row][column] = K (A operand, 16 rows x 32 channels) x q (B operand); a lane has four rows of one column.
@@ -678,7 +549,6 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttent
   *reinterpret_cast<bf16x2*>(p.out + (((int64_t)layer * p.total_new + s.first + token) * p.n_q_heads + h) * kHeadDim + 2 * lane) = result;
 }
 
-constexpr int kMostRowCols = 32;
 int row_cols(int64_t cols) { return cols <= 8 ? 8 : (cols <= 16 ? 16 : 32); }
 
 // How a call of up to 32 columns is run: a function of the descriptors alone, which the workspace follows.
@@ -733,7 +603,8 @@ int check_attention(const dapq_pages* pages, const dapq_step* step) {
                DAPQ_ERR_UNSUPPORTED, "q strides of the step must be non-negative multiples of 8 elements (row >= 128)");
   DAPQ_REQUIRE(isfinite(step->scale) && step->scale > 0.0f, DAPQ_ERR_INVALID_ARG, "scale must be finite and > 0");
   DAPQ_REQUIRE(isfinite(step->softcap) && step->softcap >= 0.0f, DAPQ_ERR_INVALID_ARG, "softcap must be finite and >= 0");
-  DAPQ_REQUIRE(step->n_q_heads <= 65535, DAPQ_ERR_UNSUPPORTED, "n_q_heads (%d) exceeds 65535", step->n_q_heads);
+  DAPQ_REQUIRE(step->n_q_heads <= 65535 && step->total_new * step->n_q_heads < (int64_t)1 << 31, DAPQ_ERR_UNSUPPORTED,
+               "n_q_heads (%d) exceeds 65535, or total_new (%lld) query rows of all heads 2^31", step->n_q_heads, (long long)step->total_new);
   return DAPQ_OK;
 }
 
@@ -745,7 +616,7 @@ using namespace dapq;
 extern "C" DAPQ_API size_t dapq_paged_attention_workspace_bytes(const dapq_pages* pages, const dapq_step* step) {
   if (check_attention(pages, step) != DAPQ_OK) return 0;
   const int64_t cols = (int64_t)step->max_new * (step->n_q_heads / pages->n_kv_heads);
-  if (cols > kMostRowCols) return 256;
+  if (cols > kMostRowCols) return turn_workspace_bytes(pages, step);
   return align_up((size_t)row_plan(pages, row_cols(cols)).groups * 2 * row_cols(cols) * (kHeadDim + 2) * sizeof(float), 256);
 }
 
@@ -773,8 +644,6 @@ extern "C" DAPQ_API int dapq_paged_attention(const dapq_pages* pages, const dapq
   p.each_new = (int32_t)(step->total_new / pages->batch);
   p.max_new = step->max_new;
   p.n_q_heads = step->n_q_heads;
-  p.scale = step->scale;
-  p.softcap = step->softcap;
   p.parts = static_cast<float*>(workspace);
   p.group = step->n_q_heads / pages->n_kv_heads;
   p.items = pages->n_layers * pages->n_kv_heads;
@@ -784,9 +653,5 @@ extern "C" DAPQ_API int dapq_paged_attention(const dapq_pages* pages, const dapq
   p.c = step->softcap > 0.0f ? step->scale / step->softcap : step->scale * kLog2e;
   const int64_t cols = (int64_t)step->max_new * p.group;
   if (cols <= kMostRowCols) return launch_rows(pages, p, row_cols(cols), static_cast<hipStream_t>(stream));
-  hipLaunchKernelGGL(pages->format == DAPQ_PAGES_FP4 ? paged_attention_kernel<true> : paged_attention_kernel<false>,
-                     dim3((unsigned)step->total_new, (unsigned)step->n_q_heads, (unsigned)pages->n_layers), dim3(64), 0,
-                     static_cast<hipStream_t>(stream), p);
-  DAPQ_HIP_LAUNCH_CHECK("paged_attention_kernel");
-  return DAPQ_OK;
+  return launch_turn(pages, step, p, static_cast<hipStream_t>(stream));
 }

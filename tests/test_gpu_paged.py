@@ -271,7 +271,7 @@ def test_attention_of_no_numbers():
 
 
 @pytest.mark.parametrize("group,new", [(1, 1), (4, 1), (2, 3), (8, 2), (4, 7), (2, 60)])
-def test_values_that_are_not_finite(group, new):
+def test_values_that_are_not_finite(group, new):  # (2 x 60: turns)
     """An infinite value or a NaN among the values of the new tokens reaches the tokens from its own on; what nobody sees reaches nobody."""
     rng = np.random.default_rng(60 + new)
     before = 45
@@ -308,6 +308,32 @@ def test_tokens_past_max_new_are_left_out(new):
     seen = list(range(2)) + list(range(2, 9))
     assert (np.abs(got - want) <= attention_bound(want, weighted, size, 100))[0, seen].all()
     assert np.isnan(got[0, 9:]).all()                            # (what the buffer held)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("heads,group,page_rows,lengths,new", [
+    (1, 4, 16, [1000], [16]), (2, 1, 64, [700, 0, 130], [33, 50, 200]), (1, 8, 32, [0], [129]), (3, 5, 16, [64, 1], [64, 63]),
+    (1, 2, 128, [0] * 70, [b % 5 * 20 for b in range(70)])])
+def test_turns(fmt, heads, group, page_rows, lengths, new):
+    """Blocks of columns that end in a token, rows shared out and not, tiles and pages of all sizes, a page missing."""
+    rng = np.random.default_rng(500 + heads)
+    rows = [h + n for h, n in zip(lengths, new)]
+    cache = Cache(rng, fmt, 1, heads, page_rows, rows).fill(rng, rows, gain=2.0)
+    if rows[0] > 3 * page_rows:
+        cache.table[0, 2] = -1
+    cache.to_device()
+    check_attention(cache, lengths, new, normal_bits(rng, 1, sum(new), heads * group, 128), softcap=15.0 if heads == 3 else 0.0, ragged=len(new) > 1)
+
+
+def test_turns_past_max_new_are_left_out():
+    rng = np.random.default_rng(18)
+    cache = Cache(rng, "bf16", 1, 1, 16, [160, 180]).fill(rng, [160, 180]).to_device()
+    q = normal_bits(rng, 1, 150, 4, 128)
+    got = attend(cache, [30, 30], [60, 90], q, max_new=35)
+    want, weighted, size = PO.attention(cache.pool, cache.table, [30, 30], [0, 60, 150], O.bf16_bits_to_f64(q), SCALE)
+    seen = list(range(35)) + list(range(60, 95))
+    assert (np.abs(got - want) <= attention_bound(want, weighted, size, 140))[0, seen].all()
+    assert np.isnan(got[0, 35:60]).all() and np.isnan(got[0, 95:]).all()
 
 
 def test_many_rows_are_the_mean_of_their_values():
