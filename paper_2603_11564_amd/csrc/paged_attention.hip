@@ -77,7 +77,7 @@ struct Part {
 //            V is transposed in registers: a lane loads the same 8 channels of 8 rows.
 // BLOCKS: blocks of 16 columns; 0: up to 8 columns, whose leading and following parts take the two halves of one block.
 // SPLIT: a workgroup has its length of the axis; else an item (and nothing is to be joined).
-template <bool FP4, int BLOCKS, bool CAP, bool SPLIT>
+template <bool FP4, int BLOCKS, int CAP, bool SPLIT>
 __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_rows_kernel(PagedAttentionParams p) {
   touch_args<sizeof(PagedAttentionParams)>();
   constexpr bool kHalf = BLOCKS == 0;
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
         if (partial) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const bool there = row0 + 16 * (e >> 2) + 4 * kg + (e & 3) < vis[t] && now.ok[e >> 2];
+            const bool there = (row0 + 16 * (e >> 2) + 4 * kg + (e & 3) < vis[t]) & now.ok[e >> 2];
             seen[t] |= there;
             if (!there) x[e] = -INFINITY;
           }
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
         float m = x[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) m = fmaxf(m, x[e]);
-        if (!CAP) m *= p.c;
+        if (CAP == kNoCap) m *= p.c;
         if (__any(m > ref[t] + kHeadroom)) {
           m = fmaxf(m, __shfl_xor(m, 16, 64));
           m = fmaxf(m, __shfl_xor(m, 32, 64));
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
         unsigned w[8], w2[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float y = __builtin_amdgcn_exp2f(CAP ? x[e] - ref[t] : fmaf(x[e], p.c, -ref[t]));
+          const float y = __builtin_amdgcn_exp2f(CAP != kNoCap ? x[e] - ref[t] : fmaf(x[e], p.c, -ref[t]));
           sum[t] += y;
           // what the leading part leaves, and 2^-22 of the weight, which keeps it from 0 where a value is infinite
           const float rest = fmaf(y, kHalf ? rest_factor : 1.0f + 0x1p-22f, -__uint_as_float(__float_as_uint(y) & (kHalf ? rest_mask : 0xffff0000u)));
@@ -569,7 +569,9 @@ RowPlan row_plan(const dapq_pages* p, int cols) {
 template <bool FP4, int BLOCKS, bool SPLIT>
 int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, hipStream_t stream) {
   constexpr int kCols = BLOCKS == 0 ? 8 : 16 * BLOCKS, kBytes = kRowWaves * (BLOCKS == 0 ? 1 : BLOCKS) * 16 * (kHeadDim + 2) * 4 + (BLOCKS == 2 ? 8192 : 0);
-  auto kernel = p.cap > 0.0f ? paged_rows_kernel<FP4, BLOCKS, true, SPLIT> : paged_rows_kernel<FP4, BLOCKS, false, SPLIT>;
+  const Cap cap = cap_of(p);
+  auto kernel = cap == kNoCap ? paged_rows_kernel<FP4, BLOCKS, kNoCap, SPLIT>
+                              : (cap == kSmallCap ? paged_rows_kernel<FP4, BLOCKS, kSmallCap, SPLIT> : paged_rows_kernel<FP4, BLOCKS, kLargeCap, SPLIT>);
   const int rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), kBytes);
   if (rc != DAPQ_OK) return rc;
   const unsigned items = (unsigned)(pages->batch * p.items);  // (below 2^24)

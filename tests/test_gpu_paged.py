@@ -211,6 +211,15 @@ def test_attention(fmt, softcap, case):
     check_attention(cache, lengths, new, q, softcap, ragged=len(set(new)) > 1, pads=(8, 16) if case % 2 else (0, 0))
 
 
+@pytest.mark.parametrize("softcap", [0.01, 1.0, 64.0, 65.0, 300.0, 1e6, 1e30])
+@pytest.mark.parametrize("new", [1, 9])
+def test_caps_of_all_sizes(softcap, new):
+    """Scores far above the cap, around it and far below it (there the cap changes nothing)."""
+    rng = np.random.default_rng(71)
+    cache = Cache(rng, "bf16", 1, 1, 32, [150 + new]).fill(rng, [150 + new], gain=3.0).to_device()
+    check_attention(cache, [150], [new], normal_bits(rng, 1, new, 4, 128), softcap, scale=0.5)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("new", [[1, 1, 1, 1], [40, 3, 33, 20]])
 def test_attention_with_pages_missing(fmt, new):
