@@ -300,7 +300,7 @@ int dapq_decode_attention(const dapq_shape* shape, const void* q_decode, const v
 enum { DAPQ_PAGES_BF16 = 0, DAPQ_PAGES_FP4 = 1 };
 typedef struct dapq_pages {
   int32_t n_layers;
-  int32_t batch;          /* sequences of the table; dapq_paged_gather and dapq_paged_read take up to 32767 */
+  int32_t batch;          /* sequences of the table; dapq_paged_gather and dapq_paged_read take up to 65535 */
   int32_t n_kv_heads;
   int32_t head_dim;       /* 128 */
   int32_t format;         /* DAPQ_PAGES_* */

@@ -52,6 +52,10 @@ int check_step(const dapq_pages* p, const dapq_step* s) {
 
 namespace {
 
+// Bytes moved from which rows go past the caches, as dapq_gather's do: us without -> with hints, 983 rows of 32 layers (258 MB) 53.0 -> 46.0 (5.6 TB/s),
+// 512 rows of 8 prompts and 32 layers into 4 bits and back out 279 -> 261, 16 sequences of 512..2048 rows, 8 layers, read (1.5 GB) 293 -> 263 (5.8 TB/s).
+constexpr int64_t kStreamOut = (int64_t)8 << 20, kStreamIn = (int64_t)192 << 20, kStreamRead = (int64_t)8 << 20;
+
 bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0; }
 bool aligned16(const void* a, const void* b) { return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15) == 0; }
 
@@ -63,21 +67,33 @@ constexpr int kXor1 = 0xB1, kXor2 = 0x4E;                               // lanes
 constexpr int kRor1 = 0x121, kRor2 = 0x122, kRor4 = 0x124, kRor8 = 0x128;  // of 16 lanes
 __device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
 
+// STREAM: past the caches.
+template <bool STREAM, typename T>
+__device__ __forceinline__ void put(T* at, T x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(x, at);
+  else *at = x;
+}
+template <bool STREAM, typename T>
+__device__ __forceinline__ T get(const T* at) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(at);
+  else return *at;
+}
+
 // A row of 16 lanes with 8 channels each into the pool.
-template <bool FP4>
+template <bool FP4, bool STREAM>
 __device__ __forceinline__ void put_row16(uint8_t* rows, uint8_t* scales, int64_t row, int ch, u32x4 x) {
   if constexpr (!FP4) {
-    *reinterpret_cast<u32x4*>(rows + row * kRowBytes + ch * 16) = x;
+    put<STREAM>(reinterpret_cast<u32x4*>(rows + row * kRowBytes + ch * 16), x);
   } else {
     unsigned m = larger(larger(larger_magnitude(x[0]), larger_magnitude(x[1])), larger(larger_magnitude(x[2]), larger_magnitude(x[3])));
     m = larger(m, dpp<kXor1>(m));
     m = larger(m, dpp<kXor2>(m));
     const unsigned s = fp4_scale_byte(m);
-    *reinterpret_cast<unsigned*>(rows + row * kFp4RowBytes + ch * 4) = fp4_pack8(x, s);
+    put<STREAM>(reinterpret_cast<unsigned*>(rows + row * kFp4RowBytes + ch * 4), fp4_pack8(x, s));
     unsigned all = s << (8 * (ch >> 2));
     all |= dpp<kRor4>(all);
     all |= dpp<kRor8>(all);
-    if (ch == 0) *reinterpret_cast<unsigned*>(scales + row * 4) = all;
+    if (ch == 0) put<STREAM>(reinterpret_cast<unsigned*>(scales + row * 4), all);
   }
 }
 
@@ -91,15 +107,16 @@ struct PagedGatherParams {
   int32_t batch, budget, seq_len;  // seq_len: dense batches
 };
 
-// As gather_kernel: 16 lanes move a row with one 16-byte load each, two rows to a lane group.
-template <bool FP4>
+// As gather_kernel, 16 lanes move a row with one 16-byte load each; a lane group has two rows, and K and V of each, whose place is looked up once.
+// STREAM_IN, STREAM_OUT: hints of the loads and stores of rows.
+template <bool FP4, bool STREAM_IN, bool STREAM_OUT>
 __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherParams p) {
+  touch_args<sizeof(PagedGatherParams)>();
   constexpr int ROWS = 2;
   const int ch = threadIdx.x & 15;
   const int slot0 = blockIdx.x * (16 * ROWS) + (threadIdx.x >> 4);
   const int layer = blockIdx.y / p.pool.n_kv_heads, kv = blockIdx.y - layer * p.pool.n_kv_heads;
-  const int seq = blockIdx.z >> 1;
-  const bool is_v = blockIdx.z & 1;
+  const int seq = blockIdx.z;
   const int64_t head = ((int64_t)layer * p.batch + seq) * p.pool.n_kv_heads + kv;
   const int n = p.count[head] < p.budget ? p.count[head] : p.budget;
   if (slot0 >= n) return;
@@ -112,21 +129,30 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherParams p) 
     start = p.cu_seqlens[seq];
     L = p.cu_seqlens[seq + 1] - (int)start;
   }
-  const uint16_t* base = is_v ? p.v + layer * p.v_stride_layer + seq * p.v_stride_seq + kv * p.v_stride_head
-                              : p.k + layer * p.k_stride_layer + seq * p.k_stride_seq + kv * p.k_stride_head;
-  const int64_t stride_token = is_v ? p.v_stride_token : p.k_stride_token;
+  const uint16_t* k = p.k + layer * p.k_stride_layer + seq * p.k_stride_seq + kv * p.k_stride_head;
+  const uint16_t* v = p.v + layer * p.v_stride_layer + seq * p.v_stride_seq + kv * p.v_stride_head;
   int j[ROWS];
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) j[r] = slot0 + 16 * r < n ? p.idx[head * p.budget + slot0 + 16 * r] : -1;
-  u32x4 x[ROWS];
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r)
-    x[r] = j[r] >= 0 && j[r] < L ? reinterpret_cast<const u32x4*>(base + (start + j[r]) * stride_token)[ch] : u32x4{0, 0, 0, 0};
+  int64_t to[ROWS];
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
-    if (j[r] < 0 || j[r] >= L) continue;  // (the 16 lanes of a row agree)
-    const int64_t row = find_row(p.pool, layer, seq, kv, slot0 + 16 * r);
-    if (row >= 0) put_row16<FP4>(is_v ? p.pool.v : p.pool.k, is_v ? p.pool.v_scales : p.pool.k_scales, row, ch, x[r]);
+    const int slot = slot0 + 16 * r;
+    j[r] = slot < n ? p.idx[head * p.budget + slot] : -1;
+    to[r] = slot < n ? find_row(p.pool, layer, seq, kv, slot) : -1;
+  }
+  u32x4 x[ROWS][2];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    x[r][0] = x[r][1] = u32x4{0, 0, 0, 0};
+    if (j[r] >= 0 && j[r] < L && to[r] >= 0) {  // (the 16 lanes of a row agree)
+      x[r][0] = get<STREAM_IN>(reinterpret_cast<const u32x4*>(k + (start + j[r]) * p.k_stride_token) + ch);
+      x[r][1] = get<STREAM_IN>(reinterpret_cast<const u32x4*>(v + (start + j[r]) * p.v_stride_token) + ch);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (j[r] < 0 || j[r] >= L || to[r] < 0) continue;
+    put_row16<FP4, STREAM_OUT>(p.pool.k, p.pool.k_scales, to[r], ch, x[r][0]);
+    put_row16<FP4, STREAM_OUT>(p.pool.v, p.pool.v_scales, to[r], ch, x[r][1]);
   }
 }
 
@@ -168,6 +194,7 @@ __device__ __forceinline__ bool find_token(const int32_t* cu_new, int batch, int
 // dapq_rope_apply does, and has the two that it needs from other lanes.
 template <bool FP4>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) {
+  touch_args<sizeof(PagedAppendParams)>();
   const int lane = threadIdx.x & 63, c = lane & 31;
   const int r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int layer = blockIdx.z;
@@ -184,6 +211,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) 
   uint8_t* rows = is_v ? p.pool.v : p.pool.k;
   uint8_t* scales = is_v ? p.pool.v_scales : p.pool.k_scales;
   const bool rotate = !is_v && p.positions != nullptr;
+  const int own = lane >> 5;  // of two heads
+  auto source = [&](int hd) { return reinterpret_cast<const unsigned*>(src + (int64_t)(hd < hd1 ? hd : hd1 - 1) * stride_head) + c; };
+  unsigned a = source(hd0 + own)[0], b = source(hd0 + own)[32];  // (on their way while the angle is evaluated)
   double sn0 = 0, cs0 = 1, sn1 = 0, cs1 = 1;
   if (rotate) {
     double sn, cs;
@@ -194,10 +224,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) 
     sn1 = __shfl(sn, a1, 64);
     cs1 = __shfl(cs, a1, 64);
   }
-  for (int hd = hd0 + (lane >> 5); hd - (lane >> 5) < hd1; hd += 2) {
+  for (int hd = hd0 + own; hd - own < hd1; hd += 2) {
     const bool mine = hd < hd1;
-    const unsigned* at = reinterpret_cast<const unsigned*>(src + (int64_t)(mine ? hd : hd1 - 1) * stride_head) + c;
-    unsigned a = at[0], b = at[32];
+    const unsigned next_a = source(hd + 2)[0], next_b = source(hd + 2)[32];
     if (rotate) {
       auto lo = [](unsigned x) { return bf16_to_f64((uint16_t)x); };
       auto hi = [](unsigned x) { return bf16_to_f64((uint16_t)(x >> 16)); };
@@ -241,6 +270,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) 
         scales[row * 4 + 2 + (c >> 4)] = (uint8_t)sb;
       }
     }
+    a = next_a;
+    b = next_b;
   }
 }
 
@@ -252,28 +283,45 @@ struct PagedReadParams {
   int32_t batch, max_rows;
 };
 
-// 16 lanes to a row, two rows to a lane group.
-template <bool FP4>
+// 16 lanes to a row, two rows of K and of V to a lane group.
+template <bool FP4, bool STREAM>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadParams p) {
+  touch_args<sizeof(PagedReadParams)>();
   constexpr int ROWS = 2;
   const int ch = threadIdx.x & 15;
   const int layer = blockIdx.y / p.pool.n_kv_heads, kv = blockIdx.y - layer * p.pool.n_kv_heads;
-  const int seq = blockIdx.z >> 1;
-  const bool is_v = blockIdx.z & 1;
-  const int n = p.lengths[seq] < p.max_rows ? p.lengths[seq] : p.max_rows;
+  const int seq = blockIdx.z;
   const int i0 = blockIdx.x * (16 * ROWS) + (threadIdx.x >> 4);
-  const uint8_t* rows = is_v ? p.pool.v : p.pool.k;
-  const uint8_t* scales = is_v ? p.pool.v_scales : p.pool.k_scales;
-  uint16_t* out = (is_v ? p.v_out : p.k_out) + (((int64_t)layer * p.batch + seq) * p.pool.n_kv_heads + kv) * p.max_rows * kHeadDim;
+  const int n = p.lengths[seq] < p.max_rows ? p.lengths[seq] : p.max_rows;
+  if (i0 >= n) return;
+  const int64_t out = ((((int64_t)layer * p.batch + seq) * p.pool.n_kv_heads + kv) * p.max_rows + i0) * kHeadDim + ch * 8;
+  int64_t row[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) row[r] = i0 + 16 * r < n ? find_row(p.pool, layer, seq, kv, i0 + 16 * r) : -1;
+  u32x4 x[ROWS][2];
+  unsigned scale[ROWS][2];
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
-    const int i = i0 + 16 * r;
-    const int64_t row = i < n ? find_row(p.pool, layer, seq, kv, i) : -1;
-    if (row < 0) continue;
-    u32x4 x;
-    if constexpr (FP4) x = fp4_unpack8(*reinterpret_cast<const unsigned*>(rows + row * kFp4RowBytes + ch * 4), fp4_scale(scales[row * 4 + (ch >> 2)]));
-    else x = *reinterpret_cast<const u32x4*>(rows + row * kRowBytes + ch * 16);
-    *reinterpret_cast<u32x4*>(out + (int64_t)i * kHeadDim + ch * 8) = x;
+    if (row[r] < 0) continue;
+    if constexpr (FP4) {
+      x[r][0][0] = *reinterpret_cast<const unsigned*>(p.pool.k + row[r] * kFp4RowBytes + ch * 4);
+      x[r][1][0] = *reinterpret_cast<const unsigned*>(p.pool.v + row[r] * kFp4RowBytes + ch * 4);
+      scale[r][0] = p.pool.k_scales[row[r] * 4 + (ch >> 2)];
+      scale[r][1] = p.pool.v_scales[row[r] * 4 + (ch >> 2)];
+    } else {
+      x[r][0] = get<STREAM>(reinterpret_cast<const u32x4*>(p.pool.k + row[r] * kRowBytes + ch * 16));
+      x[r][1] = get<STREAM>(reinterpret_cast<const u32x4*>(p.pool.v + row[r] * kRowBytes + ch * 16));
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (row[r] < 0) continue;
+    if constexpr (FP4) {
+      x[r][0] = fp4_unpack8(x[r][0][0], fp4_scale(scale[r][0]));
+      x[r][1] = fp4_unpack8(x[r][1][0], fp4_scale(scale[r][1]));
+    }
+    put<STREAM>(reinterpret_cast<u32x4*>(p.k_out + out + 16 * r * kHeadDim), x[r][0]);
+    put<STREAM>(reinterpret_cast<u32x4*>(p.v_out + out + 16 * r * kHeadDim), x[r][1]);
   }
 }
 
@@ -307,13 +355,19 @@ extern "C" DAPQ_API int dapq_paged_gather(const dapq_shape* shape, const dapq_pa
   p.batch = shape->batch;
   p.budget = budget;
   p.seq_len = (int32_t)(shape->total_tokens / shape->batch);
-  DAPQ_REQUIRE(shape->batch <= 32767, DAPQ_ERR_UNSUPPORTED, "batch (%d) exceeds 32767", shape->batch);
+  DAPQ_REQUIRE(shape->batch <= 65535, DAPQ_ERR_UNSUPPORTED, "batch (%d) exceeds 65535", shape->batch);
   // no more rows than the table has a place for
   const int64_t rows = (int64_t)pages->max_pages * pages->page_rows;
   const unsigned blocks = (unsigned)(((budget < rows ? budget : rows) + 31) / 32);
+  // bytes read and written where every head keeps its whole budget
+  const int64_t moved = (int64_t)shape->n_layers * shape->batch * shape->n_kv_heads * (budget < rows ? budget : rows) * 2 *
+                        (kRowBytes + (pages->format == DAPQ_PAGES_FP4 ? kFp4RowBytes + 4 : kRowBytes));
   DAPQ_REQUIRE((uint64_t)blocks * 256 < (uint64_t)1 << 32, DAPQ_ERR_UNSUPPORTED, "budget (%d) is too large", budget);
-  hipLaunchKernelGGL(pages->format == DAPQ_PAGES_FP4 ? paged_gather_kernel<true> : paged_gather_kernel<false>,
-                     dim3(blocks, (unsigned)(shape->n_layers * shape->n_kv_heads), (unsigned)shape->batch * 2), dim3(256), 0,
+  const bool fp4 = pages->format == DAPQ_PAGES_FP4;
+  auto kernel = fp4 ? paged_gather_kernel<true, false, false> : paged_gather_kernel<false, false, false>;
+  if (moved >= kStreamOut) kernel = fp4 ? paged_gather_kernel<true, false, true> : paged_gather_kernel<false, false, true>;
+  if (moved >= kStreamIn) kernel = fp4 ? paged_gather_kernel<true, true, true> : paged_gather_kernel<false, true, true>;
+  hipLaunchKernelGGL(kernel, dim3(blocks, (unsigned)(shape->n_layers * shape->n_kv_heads), (unsigned)shape->batch), dim3(256), 0,
                      static_cast<hipStream_t>(stream), p);
   DAPQ_HIP_LAUNCH_CHECK("paged_gather_kernel");
   return DAPQ_OK;
@@ -350,7 +404,10 @@ extern "C" DAPQ_API int dapq_paged_append(const dapq_pages* pages, const dapq_st
   p.each_new = (int32_t)(step->total_new / pages->batch);
   p.max_new = step->max_new;
   p.pairing = pairing;
-  p.run = 8;
+  // Heads of a wave: the angles of a row are worth sharing, but a small call wants a wave for every two heads (64 tokens, 8 heads, in 4 bits with reading
+  // back: 11.0 us in runs of eight, 9.8 in runs of two).
+  p.run = 2;
+  while (p.run < 32 && p.run < pages->n_kv_heads && step->total_new * pages->n_layers * ((pages->n_kv_heads + 2 * p.run - 1) / (2 * p.run)) >= 2048) p.run *= 2;
   p.k_runs = (pages->n_kv_heads + p.run - 1) / p.run;
   hipLaunchKernelGGL(pages->format == DAPQ_PAGES_FP4 ? paged_append_kernel<true> : paged_append_kernel<false>,
                      dim3((unsigned)((step->total_new + 3) / 4), (unsigned)(2 * p.k_runs), (unsigned)pages->n_layers), dim3(256), 0,
@@ -365,7 +422,7 @@ extern "C" DAPQ_API int dapq_paged_read(const dapq_pages* pages, const int32_t* 
   DAPQ_REQUIRE(lengths != nullptr && k_out != nullptr && v_out != nullptr, DAPQ_ERR_INVALID_ARG, "lengths, k_out and v_out must not be NULL");
   DAPQ_REQUIRE(max_rows >= 1, DAPQ_ERR_INVALID_ARG, "max_rows (%d) must be >= 1", max_rows);
   DAPQ_REQUIRE(aligned16(k_out, v_out), DAPQ_ERR_UNSUPPORTED, "k_out and v_out must be 16-byte aligned");
-  DAPQ_REQUIRE(pages->batch <= 32767, DAPQ_ERR_UNSUPPORTED, "batch (%d) exceeds 32767", pages->batch);
+  DAPQ_REQUIRE(pages->batch <= 65535, DAPQ_ERR_UNSUPPORTED, "batch (%d) exceeds 65535", pages->batch);
   PagedReadParams p;
   p.pool = page_pool(pages);
   p.lengths = lengths;
@@ -376,8 +433,11 @@ extern "C" DAPQ_API int dapq_paged_read(const dapq_pages* pages, const int32_t* 
   const int64_t rows = (int64_t)pages->max_pages * pages->page_rows;  // (below 2^30: 2^33 threads would be too many)
   const uint64_t blocks = (uint64_t)(((max_rows < rows ? max_rows : rows) + 31) / 32);
   DAPQ_REQUIRE(blocks * 256 < (uint64_t)1 << 32, DAPQ_ERR_UNSUPPORTED, "max_rows (%d) is too large", max_rows);
-  hipLaunchKernelGGL(pages->format == DAPQ_PAGES_FP4 ? paged_read_kernel<true> : paged_read_kernel<false>,
-                     dim3((unsigned)blocks, (unsigned)(pages->n_layers * pages->n_kv_heads), (unsigned)pages->batch * 2), dim3(256), 0,
+  const int64_t moved = (int64_t)pages->n_layers * pages->batch * pages->n_kv_heads * (max_rows < rows ? max_rows : rows) * 2 *
+                        (kRowBytes + (pages->format == DAPQ_PAGES_FP4 ? kFp4RowBytes + 4 : kRowBytes));
+  auto kernel = pages->format == DAPQ_PAGES_FP4 ? (moved >= kStreamRead ? paged_read_kernel<true, true> : paged_read_kernel<true, false>)
+                                                : (moved >= kStreamRead ? paged_read_kernel<false, true> : paged_read_kernel<false, false>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)(pages->n_layers * pages->n_kv_heads), (unsigned)pages->batch), dim3(256), 0,
                      static_cast<hipStream_t>(stream), p);
   DAPQ_HIP_LAUNCH_CHECK("paged_read_kernel");
   return DAPQ_OK;

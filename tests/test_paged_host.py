@@ -111,7 +111,7 @@ REFUSED = [
     (lambda: gather(idx=N), ERR_INVALID, "must not be NULL"), (lambda: gather(count=N), ERR_INVALID, "must not be NULL"),
     (lambda: gather(budget=0), ERR_INVALID, r"budget \(0\)"), (lambda: gather(k=At(2)), ERR_UNSUPPORTED, "aligned"),
     (lambda: gather(s=shape(k_strides=(0, 0, 0, 4))), ERR_UNSUPPORTED, "k strides"),
-    (lambda: gather(s=shape(batch=40000, total_tokens=80000), p=pages(batch=40000)), ERR_UNSUPPORTED, "32767"),
+    (lambda: gather(s=shape(batch=70000, total_tokens=140000), p=pages(batch=70000)), ERR_UNSUPPORTED, "65535"),
     (lambda: append(k=N), ERR_INVALID, "k_new"), (lambda: append(v=N), ERR_INVALID, "v_new"), (lambda: append(v=At(8)), ERR_UNSUPPORTED, "aligned"),
     (lambda: append(pairing=2), ERR_INVALID, "pairing"), (lambda: append(theta=0.0), ERR_INVALID, "theta"),
     (lambda: append(theta=float("nan")), ERR_INVALID, "theta"), (lambda: append(s=step(lengths=N)), ERR_INVALID, "lengths"),
@@ -123,7 +123,7 @@ REFUSED = [
     (lambda: append(s=step(max_new=-1)), ERR_INVALID, "negative"), (lambda: append(s=step(total_new=(1 << 25) + 2)), ERR_UNSUPPORTED, "2\\^25"),
     (lambda: read(lengths=N), ERR_INVALID, "lengths"), (lambda: read(k=N), ERR_INVALID, "k_out"), (lambda: read(v=N), ERR_INVALID, "v_out"),
     (lambda: read(rows=0), ERR_INVALID, r"max_rows \(0\)"), (lambda: read(k=At(8)), ERR_UNSUPPORTED, "aligned"),
-    (lambda: read(p=pages(batch=40000)), ERR_UNSUPPORTED, "32767"),
+    (lambda: read(p=pages(batch=70000)), ERR_UNSUPPORTED, "65535"),
     (lambda: read(p=pages(page_rows=1024, max_pages=(1 << 20) - 1), rows=1 << 30), ERR_UNSUPPORTED, "too large"),
     (lambda: attention(q=N), ERR_INVALID, "q and out"), (lambda: attention(out=N), ERR_INVALID, "q and out"),
     (lambda: attention(work=N), ERR_INVALID, "workspace is NULL"), (lambda: attention(work=At(16)), ERR_UNSUPPORTED, "256-byte"),
