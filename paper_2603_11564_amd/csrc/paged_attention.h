@@ -16,8 +16,8 @@ struct PagedAttentionParams {
   int64_t q_stride_layer, q_stride_row, q_stride_head;
   float* parts;  // of the workspace
   int32_t batch, total_new, each_new, max_new, n_q_heads;
-  int32_t group, items, groups, least_share;  // query heads of a KV head; layers * Hkv; workgroups of the row kernel; fewest tiles of one
-  float inv_group, inv_items, inv_groups;
+  int32_t group, items, groups, spare;  // query heads of a KV head; layers * Hkv; of the row kernel: workgroups, and those that items leave
+  float inv_group, inv_items, inv_spare;
   float c, cap;       // c: scale * log2(e), with a cap scale / softcap; cap: softcap * log2(e)
 };
 

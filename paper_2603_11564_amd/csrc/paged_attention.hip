@@ -10,9 +10,11 @@ constexpr int kRowWaves = 4;  // of a workgroup
 constexpr unsigned kNoPage = 0xffffffffu;
 
 // ---- how the row kernel shares out the rows ---------------------------------------------------------------------------
-// An item is one KV head of one sequence and layer, with all columns (new tokens x query heads of the KV head).  The tiles of all items, sequence by
-// sequence, are one axis; every workgroup has the same length of it, so that sequences of any lengths share the chip evenly.  An
-// item that lies in one workgroup is finished there; the parts of the others meet in a second kernel, in order.
+// An item is one KV head of one sequence and layer, with all columns (new tokens x query heads of the KV head).  Where there are many items a
+// workgroup has one each.  Where there are few and long ones, every item is cut into parts of about the same length (`share`), as many as the chip holds
+// workgroups in all, so that sequences of any lengths share it evenly; a part has a workgroup, and a second kernel joins an item's parts, in order.
+// (Shares of one long axis of all tiles, with workgroups that go on into the next item, are as even, but a second item in a workgroup starts all over:
+// 300 rows, 1 sequence 13.5 us, where a share happened to be a divisor of an item 12.1 with 1000.)
 struct Sequence {
   int first, tokens;  // its new tokens
   int before;         // rows held before them
@@ -58,11 +60,13 @@ __device__ __forceinline__ Sequence from_lane(const Sequence& s, int lane) {
 __device__ __forceinline__ int64_t divide(int64_t a, int b, float inv) {
   return a < kQuotientMax ? __builtin_amdgcn_readfirstlane(quotient((int)a, inv)) : uniform64(a / b);
 }
-// A workgroup's length of the axis: at least a tile to a wave.
-__device__ __forceinline__ int64_t share_of(const PagedAttentionParams& p, int64_t total) {
-  const int64_t share = divide(total + p.groups - 1, p.groups, p.inv_groups);
-  return share < p.least_share ? p.least_share : share;
+// The length of a part: at least a tile to a wave, and so that the parts of all items, each rounded up, are no more than the chip's workgroups: one more
+// to an item than its tiles over the share, and the items have left `spare` of them for that quotient.
+__device__ __forceinline__ int share_of(const PagedAttentionParams& p, int64_t tiles) {
+  const int64_t share = divide(tiles * p.items + p.spare - 1, p.spare, p.inv_spare);
+  return (int)(share < kRowWaves ? kRowWaves : (share < 1 << 30 ? share : 1 << 30));
 }
+__device__ __forceinline__ uint32_t parts_of(int tiles, int share) { return ((uint32_t)tiles + (uint32_t)share - 1) / (uint32_t)share; }
 
 // A part of an item in the workspace: weighted sums, references and sums of weights of its columns.
 template <int COLS>
@@ -76,7 +80,7 @@ struct Part {
 //   output   D[column][channel] += weights (A) x V (B); a weight enters as two bf16 numbers, the leading 8 bits of its significand and the next 8.
 //            V is transposed in registers: a lane loads the same 8 channels of 8 rows.
 // BLOCKS: blocks of 16 columns; 0: up to 8 columns, whose leading and following parts take the two halves of one block.
-// SPLIT: a workgroup has its length of the axis; else an item (and nothing is to be joined).
+// SPLIT: a workgroup has a part of an item; else an item (and nothing is to be joined).
 template <bool FP4, int BLOCKS, int CAP, bool SPLIT>
 __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_rows_kernel(PagedAttentionParams p) {
   touch_args<sizeof(PagedAttentionParams)>();
@@ -95,38 +99,52 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
   const unsigned rest_mask = n >= 8 ? 0xffff0000u : 0u;
   const float rest_factor = n >= 8 ? 1.0f + 0x1p-22f : 1.0f;
 
-  // this workgroup's part of the axis, and the sequence it starts in
-  int seq, item, tile0;
-  int64_t left;
+  // the entries of the table that the halves of the tile at `row` have (of the last page, past the table)
+  auto entries_of = [&](int64_t table, int64_t row, int* a, int* b) {
+    const int64_t last = p.pool.max_pages - 1, e0 = row >> p.pool.page_shift, e1 = (row + 16) >> p.pool.page_shift;
+    *a = p.pool.table[table + (e0 < last ? e0 : last)];
+    *b = p.pool.table[table + (e1 < last ? e1 : last)];
+  };
+  int entry0 = -1, entry1 = -1;
+  // this workgroup's item, and its part of it
+  int seq, item, part = 0, parts = 1;
   Sequence s;
   if constexpr (SPLIT) {
     Tiles t = tiles_of_64(p, 0, lane);
     int64_t total = from_lane(t.upto, 63);
     for (int b0 = 64; b0 < p.batch; b0 += 64) total += from_lane(tiles_of_64(p, b0, lane).upto, 63);
-    left = share_of(p, total * p.items);
-    int64_t at = (int64_t)blockIdx.x * left;  // (from the start of the 64 sequences)
-    for (seq = 0; at >= (int64_t)from_lane(t.upto, 63) * p.items;) {
-      at -= (int64_t)from_lane(t.upto, 63) * p.items;
+    const int share = share_of(p, total);
+    int at = blockIdx.x;  // (from the start of the 64 sequences)
+    uint32_t own, upto;
+    for (seq = 0;;) {
+      own = parts_of(t.own.tiles, share);
+      upto = wave_scan<OpAdd>(own);
+      const int all = (int)from_lane(upto, 63) * p.items;
+      if (at < all) break;
+      at -= all;
       seq += 64;
       if (seq >= p.batch) return;
       t = tiles_of_64(p, seq, lane);
     }
-    const int l = __builtin_ctzll(__ballot(t.upto > (uint32_t)divide(at, p.items, p.inv_items)));
+    const int l = __builtin_ctzll(__ballot(upto > (uint32_t)uniform_quotient(at, p.items, p.inv_items)));
     seq += l;
     s = from_lane(t.own, l);
-    at -= (int64_t)(from_lane(t.upto, l) - s.tiles) * p.items;
-    item = (int)divide(at, s.tiles, 1.0f / (float)s.tiles);  // layer * Hkv + head
-    tile0 = (int)(at - (int64_t)item * s.tiles);
+    parts = (int)from_lane(own, l);
+    at -= ((int)from_lane(upto, l) - parts) * p.items;
+    item = uniform_quotient(at, parts, 1.0f / (float)parts);  // layer * Hkv + head
+    part = at - item * parts;
   } else {
     seq = (int)divide(blockIdx.x, p.items, p.inv_items);
     item = blockIdx.x - seq * p.items;
+    // the first entries of the table are on their way before it is known how many of them count
+    entries_of((int64_t)seq * p.pool.max_pages, (wave + (int64_t)kRowWaves * lane) * kTile, &entry0, &entry1);
     s = uniform_sequence(p, seq);
-    tile0 = 0;
-    left = s.tiles;
+    if (s.tiles == 0) return;
   }
+  const int tile0 = SPLIT ? uniform((int)((int64_t)s.tiles * part / parts)) : 0;
+  const int tile1 = SPLIT ? uniform((int)((int64_t)s.tiles * (part + 1) / parts)) : s.tiles;
 
-  while (left > 0) {
-    const int tile1 = uniform(s.tiles - tile0 < left ? s.tiles : tile0 + (int)left);
+  {
     const int layer = item / p.pool.n_kv_heads, head = item - layer * p.pool.n_kv_heads;
     const int cols = s.tokens * g;
     // the columns of this lane: query rows as operand, and what they see
@@ -152,20 +170,17 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
     const int seen_by_all = rows_seen(p, s.before, 0), seen_by_last = rows_seen(p, s.before, s.tokens - 1);
 
     // pages of this wave's tiles, 64 tiles at a time, one to a lane
-    const int32_t* table = p.pool.table + (int64_t)seq * p.pool.max_pages;
     // as the number of 16 rows that the halves of a tile are (the rows of a pool over 16: below 2^32)
     unsigned half0 = kNoPage, half1 = kNoPage;
     auto load_pages = [&](int k) {
       const int64_t row = ((int64_t)tile0 + wave + (int64_t)kRowWaves * (k + opaque(lane))) * kTile;
-      const bool there = row < (int64_t)tile1 * kTile;
-      const int64_t last = p.pool.max_pages - 1, e0 = row >> p.pool.page_shift, e1 = (row + 16) >> p.pool.page_shift;
-      const int page0 = table[there ? (e0 < last ? e0 : last) : 0], page1 = table[there ? (e1 < last ? e1 : last) : 0];
-      auto sixteen = [&](int64_t e, int page, int64_t r) {
-        if (!there || e > last || page < 0 || page >= p.pool.n_pages) return kNoPage;
-        return (unsigned)((page_row(p.pool, layer, page, head) + (r & ((1 << p.pool.page_shift) - 1))) >> 4);
+      if (SPLIT || k > 0) entries_of((int64_t)seq * p.pool.max_pages, row, &entry0, &entry1);
+      auto sixteen = [&](int page, int64_t r) {
+        const bool there = row < (int64_t)tile1 * kTile && r >> p.pool.page_shift < p.pool.max_pages && page >= 0 && page < p.pool.n_pages;
+        return there ? (unsigned)((page_row(p.pool, layer, page, head) + (r & ((1 << p.pool.page_shift) - 1))) >> 4) : kNoPage;
       };
-      half0 = sixteen(e0, page0, row);
-      half1 = sixteen(e1, page1, row + 16);
+      half0 = sixteen(entry0, row);
+      half1 = sixteen(entry1, row + 16);
     };
     struct Rows {
       unsigned at[2];
@@ -420,8 +435,8 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
       }
     }
     __syncthreads();
-    const bool whole = !SPLIT || (tile0 == 0 && tile1 == s.tiles);
-    float* part = p.parts + ((int64_t)blockIdx.x * 2 + (tile0 == 0 ? 1 : 0)) * Part<kCols>::kFloats;
+    const bool whole = !SPLIT || parts == 1;
+    float* mine_of = p.parts + (int64_t)blockIdx.x * Part<kCols>::kFloats;
     for (int e = opaque(tid); e < cols * (kHeadDim / 2); e += 64 * kRowWaves) {
       const int col = e / (kHeadDim / 2), c = 2 * (e % (kHeadDim / 2));
       float m = -INFINITY;
@@ -449,60 +464,47 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
         result[1] = (__bf16)(m == -INFINITY ? 0.0f : o[1] / total);
         *reinterpret_cast<bf16x2*>(p.out + (((int64_t)layer * p.total_new + s.first + token) * p.n_q_heads + h) * kHeadDim + c) = result;
       } else {
-        *reinterpret_cast<f32x2*>(part + col * kHeadDim + c) = o;
+        *reinterpret_cast<f32x2*>(mine_of + col * kHeadDim + c) = o;
         if (c == 0) {
-          part[kCols * kHeadDim + col] = m;
-          part[kCols * (kHeadDim + 1) + col] = total;
+          mine_of[kCols * kHeadDim + col] = m;
+          mine_of[kCols * (kHeadDim + 1) + col] = total;
         }
       }
     }
-    if (!SPLIT) return;
-    left = uniform64(left - (tile1 - tile0));
-    tile0 = 0;
-    if (++item == p.items) {
-      item = 0;
-      do {
-        if (++seq >= p.batch) return;
-        s = uniform_sequence(p, seq);
-      } while (s.tiles == 0);
-    }
-    __syncthreads();
   }
 }
 
 // The items that several workgroups share: a workgroup per item and column, its waves take the parts in turn and meet in LDS.
-constexpr int kJoinWaves = 8;
+constexpr int kJoinWaves = 8, kJoinEarly = 4;
 template <int COLS>
 __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttentionParams p) {
   __shared__ float wave_sums[kJoinWaves][kHeadDim + 2];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int seq = (int)divide(blockIdx.x, p.items, p.inv_items), item = blockIdx.x - seq * p.items, col = blockIdx.y;
   Tiles t = tiles_of_64(p, 0, lane);
-  int64_t total = from_lane(t.upto, 63), from = 0;  // (tiles of an item)
-  Sequence s = from_lane(t.own, seq & 63);
-  if (seq < 64) from = from_lane(t.upto, seq);
-  for (int b0 = 64; b0 < p.batch; b0 += 64) {
-    t = tiles_of_64(p, b0, lane);
-    if (seq >= b0 && seq < b0 + 64) {
-      s = from_lane(t.own, seq & 63);
-      from = total + from_lane(t.upto, seq & 63);
-    }
-    total += from_lane(t.upto, 63);
+  int64_t total = from_lane(t.upto, 63);
+  for (int b0 = 64; b0 < p.batch; b0 += 64) total += from_lane(tiles_of_64(p, b0, lane).upto, 63);
+  const int share = share_of(p, total);
+  int first = 0;  // the workgroup that has the item's first part
+  for (int b0 = 0; b0 < (seq & ~63); b0 += 64) {
+    first += (int)from_lane(wave_scan<OpAdd>(parts_of(t.own.tiles, share)), 63) * p.items;
+    t = tiles_of_64(p, b0 + 64, lane);
   }
-  if (s.tiles == 0 || col >= s.tokens * p.group) return;
-  const int64_t share = share_of(p, total * p.items);
-  from = (from - s.tiles) * p.items + (int64_t)item * s.tiles;
-  const float inv = 1.0f / (float)share;
-  const int first = (int)(share < kQuotientMax ? divide(from, (int)share, inv) : from / share);
-  const int parts = (int)(share < kQuotientMax ? divide(from + s.tiles - 1, (int)share, inv) : (from + s.tiles - 1) / share) - first + 1;
-  if (parts == 1) return;
-  auto part = [&](int i) { return p.parts + ((int64_t)(first + i) * 2 + (i == 0 ? 1 : 0)) * Part<COLS>::kFloats; };
+  const Sequence s = from_lane(t.own, seq & 63);
+  const uint32_t own = parts_of(t.own.tiles, share);
+  const int parts = (int)from_lane(own, seq & 63);
+  if (parts <= 1 || col >= s.tokens * p.group) return;
+  first += ((int)from_lane(wave_scan<OpAdd>(own), seq & 63) - parts) * p.items + item * parts;
+  auto part = [&](int i) { return p.parts + (int64_t)(first + i) * Part<COLS>::kFloats; };
   float m = -INFINITY, sum = 0.0f;
   f32x2 o = {0.0f, 0.0f};
   for (int i0 = wave; i0 < parts; i0 += kJoinWaves * 64) {  // 64 parts of this wave, one to a lane
     const int mine = i0 + kJoinWaves * lane, n = (parts - i0 + kJoinWaves - 1) / kJoinWaves < 64 ? (parts - i0 + kJoinWaves - 1) / kJoinWaves : 64;
     const float r = mine < parts ? part(mine)[COLS * kHeadDim + col] : -INFINITY;
     float w = mine < parts ? part(mine)[COLS * (kHeadDim + 1) + col] : 0.0f;
+    f32x2 early[kJoinEarly];  // (their loads need no weights)
+#pragma unroll
+    for (int i = 0; i < kJoinEarly; ++i) early[i] = *reinterpret_cast<const f32x2*>(part(i0 + kJoinWaves * (i < n ? i : n - 1)) + col * kHeadDim + 2 * lane);
     float top = r;
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     const float moved = fmaxf(m, top);
@@ -513,14 +515,17 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttent
     sum = m == -INFINITY ? w : fmaf(sum, before, w);
     if (m != -INFINITY) o *= before;
     m = moved;
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const f32x2 x = *reinterpret_cast<const f32x2*>(part(i0 + kJoinWaves * i) + col * kHeadDim + 2 * lane);
+    auto add = [&](int i, f32x2 x) {
       const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
-      if (__builtin_amdgcn_readlane(__float_as_uint(r), i) == 0xff800000u) continue;
+      if (__builtin_amdgcn_readlane(__float_as_uint(r), i) == 0xff800000u) return;
       o[0] = fmaf(fi, x[0], o[0]);
       o[1] = fmaf(fi, x[1], o[1]);
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < kJoinEarly; ++i)
+      if (i < n) add(i, early[i]);
+#pragma unroll 4
+    for (int i = kJoinEarly; i < n; ++i) add(i, *reinterpret_cast<const f32x2*>(part(i0 + kJoinWaves * i) + col * kHeadDim + 2 * lane));
   }
   *reinterpret_cast<f32x2*>(&wave_sums[wave][2 * lane]) = o;
   if (lane == 0) {
@@ -554,15 +559,22 @@ int row_cols(int64_t cols) { return cols <= 8 ? 8 : (cols <= 16 ? 16 : 32); }
 // How a call of up to 32 columns is run: a function of the descriptors alone, which the workspace follows.
 struct RowPlan {
   bool split;
-  int groups;
+  int groups, spare;  // workgroups of a split call; those that are left when every item has one
 };
 RowPlan row_plan(const dapq_pages* p, int cols) {
   const int64_t tiles = ((int64_t)p->max_pages * p->page_rows + kTile - 1) / kTile;  // of an item, at most
   const int64_t items = (int64_t)p->n_layers * p->batch * p->n_kv_heads;
   RowPlan plan;
-  plan.split = items < 256 && tiles > 40;
-  const int64_t groups = (tiles * items + kRowWaves - 1) / kRowWaves, chip = cols == 32 ? 512 : 768;
+  // An item takes some 6 us and `tile` for each tile of it, a workgroup's four waves one after the other; parts take `join` more, and what their bytes take
+  // of the chip.  Us, parts / items, 8 KV heads, bf16, sequences x rows: 1 x 600 10.6 / 9.7, 1 x 1000 11.9 / 13.6, 1 x 8000 17.2 / 74.3, 4 x 1000 13.0 / 14.2,
+  // 8 x 1000 15.0 / 14.4, 8 x 2000 19.4 / 22.7, 16 x 2000 34.0 / 30.0, 16 x 4000 57.5 / 55.5, 24 x 2000 47 / 37; in 4 bits 1 x 1000 11.3 / 9.8, 1 x 2000
+  // 11.5 / 15.2, 8 x 1000 12.2 / 10.0, 8 x 2000 13.7 / 15.4, 16 x 2000 16.3 / 15.6, 16 x 4000 21.2 / 26.3, 31 x 2000 20.8 / 16.2.
+  const bool fp4 = p->format == DAPQ_PAGES_FP4;
+  const double tile = fp4 ? 0.16 : 0.27, bytes = (fp4 ? 4352 : 16384) / 6.5e6, join = fp4 ? 6.5 : 5.5;
+  plan.split = items < 256 && (double)tiles * (tile - bytes * (double)items) > join;
+  const int64_t chip = cols == 32 ? 512 : 768, groups = (tiles + kRowWaves - 1) / kRowWaves * items;
   plan.groups = (int)(groups < chip ? groups : chip);
+  plan.spare = (int)(chip - items);
   return plan;
 }
 
@@ -590,8 +602,8 @@ int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, int cols
 int launch_rows(const dapq_pages* pages, PagedAttentionParams p, int cols, hipStream_t stream) {
   const RowPlan plan = row_plan(pages, cols);
   p.groups = plan.groups;
-  p.inv_groups = 1.0f / (float)plan.groups;
-  p.least_share = kRowWaves;
+  p.spare = plan.spare;
+  p.inv_spare = 1.0f / (float)plan.spare;
   if (pages->format == DAPQ_PAGES_FP4) return plan.split ? launch_rows<true, true>(pages, p, cols, stream) : launch_rows<true, false>(pages, p, cols, stream);
   return plan.split ? launch_rows<false, true>(pages, p, cols, stream) : launch_rows<false, false>(pages, p, cols, stream);
 }
@@ -619,7 +631,8 @@ extern "C" DAPQ_API size_t dapq_paged_attention_workspace_bytes(const dapq_pages
   if (check_attention(pages, step) != DAPQ_OK) return 0;
   const int64_t cols = (int64_t)step->max_new * (step->n_q_heads / pages->n_kv_heads);
   if (cols > kMostRowCols) return turn_workspace_bytes(pages, step);
-  return align_up((size_t)row_plan(pages, row_cols(cols)).groups * 2 * row_cols(cols) * (kHeadDim + 2) * sizeof(float), 256);
+  const RowPlan plan = row_plan(pages, row_cols(cols));
+  return plan.split ? align_up((size_t)plan.groups * row_cols(cols) * (kHeadDim + 2) * sizeof(float), 256) : 256;
 }
 
 extern "C" DAPQ_API int dapq_paged_attention(const dapq_pages* pages, const dapq_step* step, const void* q, void* out, void* workspace,
