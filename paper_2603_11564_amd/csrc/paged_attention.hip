@@ -474,13 +474,15 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
   }
 }
 
-// The items that several workgroups share: a workgroup per item and column, its waves take the parts in turn and meet in LDS.
+// The items that several workgroups share.  WAVES: a column has all waves of a workgroup, which take its parts in turn and meet in LDS (few items, many
+// parts), or one (32 sequences, 32 columns, 2 parts each: the whole call 150 -> 138 us).
 constexpr int kJoinWaves = 8, kJoinEarly = 4;
-template <int COLS>
+template <int COLS, int WAVES>
 __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttentionParams p) {
   __shared__ float wave_sums[kJoinWaves][kHeadDim + 2];
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int seq = (int)divide(blockIdx.x, p.items, p.inv_items), item = blockIdx.x - seq * p.items, col = blockIdx.y;
+  const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : uniform(threadIdx.x >> 6);
+  const int seq = (int)divide(blockIdx.x, p.items, p.inv_items), item = blockIdx.x - seq * p.items;
+  const int col = WAVES == 1 ? blockIdx.y * kJoinWaves + uniform(threadIdx.x >> 6) : blockIdx.y;
   Tiles t = tiles_of_64(p, 0, lane);
   int64_t total = from_lane(t.upto, 63);
   for (int b0 = 64; b0 < p.batch; b0 += 64) total += from_lane(tiles_of_64(p, b0, lane).upto, 63);
@@ -498,13 +500,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttent
   auto part = [&](int i) { return p.parts + (int64_t)(first + i) * Part<COLS>::kFloats; };
   float m = -INFINITY, sum = 0.0f;
   f32x2 o = {0.0f, 0.0f};
-  for (int i0 = wave; i0 < parts; i0 += kJoinWaves * 64) {  // 64 parts of this wave, one to a lane
-    const int mine = i0 + kJoinWaves * lane, n = (parts - i0 + kJoinWaves - 1) / kJoinWaves < 64 ? (parts - i0 + kJoinWaves - 1) / kJoinWaves : 64;
+  for (int i0 = wave; i0 < parts; i0 += WAVES * 64) {  // 64 parts of this wave, one to a lane
+    const int mine = i0 + WAVES * lane, n = (parts - i0 + WAVES - 1) / WAVES < 64 ? (parts - i0 + WAVES - 1) / WAVES : 64;
     const float r = mine < parts ? part(mine)[COLS * kHeadDim + col] : -INFINITY;
     float w = mine < parts ? part(mine)[COLS * (kHeadDim + 1) + col] : 0.0f;
     f32x2 early[kJoinEarly];  // (their loads need no weights)
 #pragma unroll
-    for (int i = 0; i < kJoinEarly; ++i) early[i] = *reinterpret_cast<const f32x2*>(part(i0 + kJoinWaves * (i < n ? i : n - 1)) + col * kHeadDim + 2 * lane);
+    for (int i = 0; i < kJoinEarly; ++i) early[i] = *reinterpret_cast<const f32x2*>(part(i0 + WAVES * (i < n ? i : n - 1)) + col * kHeadDim + 2 * lane);
     float top = r;
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     const float moved = fmaxf(m, top);
@@ -525,26 +527,28 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttent
     for (int i = 0; i < kJoinEarly; ++i)
       if (i < n) add(i, early[i]);
 #pragma unroll 4
-    for (int i = kJoinEarly; i < n; ++i) add(i, *reinterpret_cast<const f32x2*>(part(i0 + kJoinWaves * i) + col * kHeadDim + 2 * lane));
+    for (int i = kJoinEarly; i < n; ++i) add(i, *reinterpret_cast<const f32x2*>(part(i0 + WAVES * i) + col * kHeadDim + 2 * lane));
   }
-  *reinterpret_cast<f32x2*>(&wave_sums[wave][2 * lane]) = o;
-  if (lane == 0) {
-    wave_sums[wave][kHeadDim] = m;
-    wave_sums[wave][kHeadDim + 1] = sum;
-  }
-  __syncthreads();
-  if (wave != 0) return;
-  const int waves = parts < kJoinWaves ? parts : kJoinWaves;
-  m = -INFINITY;
-  for (int w = 0; w < waves; ++w) m = fmaxf(m, wave_sums[w][kHeadDim]);
-  o = f32x2{0.0f, 0.0f};
-  sum = 0.0f;
-  for (int w = 0; w < waves; ++w) {  // (in order)
-    if (wave_sums[w][kHeadDim] == -INFINITY) continue;
-    const float f = __builtin_amdgcn_exp2f(wave_sums[w][kHeadDim] - m);
-    o[0] = fmaf(f, wave_sums[w][2 * lane], o[0]);
-    o[1] = fmaf(f, wave_sums[w][2 * lane + 1], o[1]);
-    sum = fmaf(f, wave_sums[w][kHeadDim + 1], sum);
+  if constexpr (WAVES > 1) {
+    *reinterpret_cast<f32x2*>(&wave_sums[wave][2 * lane]) = o;
+    if (lane == 0) {
+      wave_sums[wave][kHeadDim] = m;
+      wave_sums[wave][kHeadDim + 1] = sum;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    const int waves = parts < WAVES ? parts : WAVES;
+    m = -INFINITY;
+    for (int w = 0; w < waves; ++w) m = fmaxf(m, wave_sums[w][kHeadDim]);
+    o = f32x2{0.0f, 0.0f};
+    sum = 0.0f;
+    for (int w = 0; w < waves; ++w) {  // (in order)
+      if (wave_sums[w][kHeadDim] == -INFINITY) continue;
+      const float f = __builtin_amdgcn_exp2f(wave_sums[w][kHeadDim] - m);
+      o[0] = fmaf(f, wave_sums[w][2 * lane], o[0]);
+      o[1] = fmaf(f, wave_sums[w][2 * lane + 1], o[1]);
+      sum = fmaf(f, wave_sums[w][kHeadDim + 1], sum);
+    }
   }
   const int layer = item / p.pool.n_kv_heads, head = item - layer * p.pool.n_kv_heads;
   const int token = quotient(col, p.inv_group), h = head * p.group + col - token * p.group;
@@ -571,8 +575,13 @@ RowPlan row_plan(const dapq_pages* p, int cols) {
   // 11.5 / 15.2, 8 x 1000 12.2 / 10.0, 8 x 2000 13.7 / 15.4, 16 x 2000 16.3 / 15.6, 16 x 4000 21.2 / 26.3, 31 x 2000 20.8 / 16.2.
   const bool fp4 = p->format == DAPQ_PAGES_FP4;
   const double tile = fp4 ? 0.16 : 0.27, bytes = (fp4 ? 4352 : 16384) / 6.5e6, join = fp4 ? 6.5 : 5.5;
-  plan.split = items < 256 && (double)tiles * (tile - bytes * (double)items) > join;
-  const int64_t chip = cols == 32 ? 512 : 768, groups = (tiles + kRowWaves - 1) / kRowWaves * items;
+  // Lengths are not known here, only the table's width: from 30 us an item on parts also keep a long sequence from outlasting the others (8 KV heads, bf16, 16
+  // sequences of 1024..8192 rows 58 / 98, 32 of them 120 / 123; 64 of 1000..4000 122 / 122).
+  plan.split = items <= 4096 && ((double)tiles * (tile - bytes * (double)items) > join || (double)tiles * tile > 30.0);
+  // At least as many workgroups as the chip holds, and enough to an item that parts come in several lengths (32 columns, 32 sequences of 1024..8192 rows, two to an
+  // item 138 us, four 131, six 134; 8 columns, 256 sequences of 4000 rows 709, 734, 751).
+  const int64_t resident = cols == 32 ? 512 : 768, wanted = (cols == 32 ? 4 : 2) * items, chip = resident > wanted ? resident : wanted;
+  const int64_t groups = (tiles + kRowWaves - 1) / kRowWaves * items;
   plan.groups = (int)(groups < chip ? groups : chip);
   plan.spare = (int)(chip - items);
   return plan;
@@ -590,7 +599,9 @@ int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, hipStrea
   hipLaunchKernelGGL(kernel, dim3(SPLIT ? (unsigned)p.groups : items), dim3(64 * kRowWaves), kBytes, stream, p);
   DAPQ_HIP_LAUNCH_CHECK("paged_rows_kernel");
   if (SPLIT) {
-    hipLaunchKernelGGL((paged_join_kernel<kCols>), dim3(items, (unsigned)(p.max_new * p.group)), dim3(64 * kJoinWaves), 0, stream, p);
+    const unsigned cols = (unsigned)(p.max_new * p.group);
+    if (items < 128) hipLaunchKernelGGL((paged_join_kernel<kCols, kJoinWaves>), dim3(items, cols), dim3(64 * kJoinWaves), 0, stream, p);
+    else hipLaunchKernelGGL((paged_join_kernel<kCols, 1>), dim3(items, (cols + kJoinWaves - 1) / kJoinWaves), dim3(64 * kJoinWaves), 0, stream, p);
     DAPQ_HIP_LAUNCH_CHECK("paged_join_kernel");
   }
   return DAPQ_OK;

@@ -211,6 +211,31 @@ def test_attention(fmt, softcap, case):
     check_attention(cache, lengths, new, q, softcap, ragged=len(set(new)) > 1, pads=(8, 16) if case % 2 else (0, 0))
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("case", range(len(ATTENTION)))
+def test_attention_through_a_wide_table(fmt, case):
+    """A table of 20000 rows a sequence, most of which have no page: the parts that rows are shared out in follow the lengths, not the table."""
+    layers, heads, group, page_rows, lengths, new = ATTENTION[case]
+    rng = np.random.default_rng(300 + case)
+    rows = [h + n for h, n in zip(lengths, new)]
+    cache = Cache(rng, fmt, layers, heads, page_rows, rows, extra_entries=20000 // page_rows).fill(rng, rows, gain=2.0).to_device()
+    check_attention(cache, lengths, new, normal_bits(rng, layers, sum(new), heads * group, 128), ragged=len(set(new)) > 1)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_long_sequence_among_many(fmt):
+    """150 sequences, one of which has most of the rows, some none: parts of all lengths, also of sequences past the first 64."""
+    rng = np.random.default_rng(301)
+    lengths = [int(n) for n in rng.integers(0, 40, 150)]
+    lengths[3], lengths[100] = 700, 2500
+    new = [int(n) for n in rng.integers(0, 3, 150)]
+    new[100] = 2
+    rows = [h + n for h, n in zip(lengths, new)]
+    cache = Cache(rng, fmt, 1, 1, 16, rows, extra_entries=1000).fill(rng, rows).to_device()
+    for group in (4, 16):
+        check_attention(cache, lengths, new, normal_bits(rng, 1, sum(new), group, 128))
+
+
 @pytest.mark.parametrize("softcap", [0.01, 1.0, 64.0, 65.0, 300.0, 1e6, 1e30])
 @pytest.mark.parametrize("new", [1, 9])
 def test_caps_of_all_sizes(softcap, new):
@@ -497,6 +522,30 @@ def test_decoding_replayed_from_a_graph(fmt):
             torch.cuda.synchronize()
         assert torch.equal(out, want[i]), i
     same_pool(cache.from_device(), eager)
+
+
+def test_two_calls_at_once():
+    """On two streams, with a workspace each, over pages that two sequences share."""
+    rng = np.random.default_rng(42)
+    cache = Cache(rng, "bf16", 1, 2, 16, [900, 900]).fill(rng, [900, 900])
+    cache.table[1] = cache.table[0]
+    cache.to_device()
+    q = [normal_bits(rng, 1, 2, 8, 128) for _ in range(2)]
+    want = [attend(cache, [898, 400], [1, 1], x) for x in q]
+    assert not np.array_equal(want[0], want[1])
+    calls = []
+    for x in q:
+        dq, strides = strided(x)
+        step = make_step([898, 400], [1, 1], False, n_q_heads=8, q_strides=strides)
+        calls.append((torch.cuda.Stream(), dq, step, torch.zeros((1, 2, 8, 128), dtype=torch.bfloat16, device="cuda"),
+                      torch.empty(D.paged_attention_workspace_bytes(cache.pages, step), dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, dq, step, out, work in calls:
+            D.dapq_paged_attention(cache.pages, step, dq, out, work, stream=stream)
+    torch.cuda.synchronize()
+    for call, ref in zip(calls, want):
+        assert np.array_equal(call[3].double().cpu().numpy(), ref)
 
 
 def test_on_another_stream():

@@ -205,8 +205,8 @@ def test_fp4_loses_at_most_half_a_step():
 def test_attention_by_hand():
     """Two rows with logits 0 and ln 3: weights 1/4 and 3/4; capped at 1 the second logit is tanh(ln 3) = 0.8."""
     pool = {"k": np.zeros((1, 1, 1, 16, 128), np.uint16), "v": np.zeros((1, 1, 1, 16, 128), np.uint16)}
-    pool["k"][0, 0, 0, 1, 0] = O.f64_to_bf16_bits(np.array([1.0]))
-    pool["v"][0, 0, 0, 0, 0] = O.f64_to_bf16_bits(np.array([4.0]))
+    pool["k"][0, 0, 0, 1, 0] = O.f64_to_bf16_bits(np.array([1.0]))[0]
+    pool["v"][0, 0, 0, 0, 0] = O.f64_to_bf16_bits(np.array([4.0]))[0]
     q = np.zeros((1, 2, 1, 128))
     q[0, :, 0, 0] = np.log(3.0)
     table = np.array([[0]], dtype=np.int32)
