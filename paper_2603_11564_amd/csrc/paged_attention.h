@@ -21,6 +21,12 @@ struct PagedAttentionParams {
   float c, cap;       // c: scale * log2(e), with a cap scale / softcap; cap: softcap * log2(e)
 };
 
+// New tokens of a sequence, at most.
+inline int32_t most_new(const dapq_pages* pages, const dapq_step* step) {
+  const int64_t n = step->cu_new == nullptr ? step->total_new / pages->batch : step->total_new;
+  return (int32_t)(step->max_new < n ? step->max_new : n);
+}
+
 // The call with more columns (new tokens x query heads of a KV head) than the row kernel takes.
 constexpr int kMostRowCols = 32;
 size_t turn_workspace_bytes(const dapq_pages* pages, const dapq_step* step);

@@ -640,7 +640,7 @@ using namespace dapq;
 
 extern "C" DAPQ_API size_t dapq_paged_attention_workspace_bytes(const dapq_pages* pages, const dapq_step* step) {
   if (check_attention(pages, step) != DAPQ_OK) return 0;
-  const int64_t cols = (int64_t)step->max_new * (step->n_q_heads / pages->n_kv_heads);
+  const int64_t cols = (int64_t)most_new(pages, step) * (step->n_q_heads / pages->n_kv_heads);
   if (cols > kMostRowCols) return turn_workspace_bytes(pages, step);
   const RowPlan plan = row_plan(pages, row_cols(cols));
   return plan.split ? align_up((size_t)plan.groups * row_cols(cols) * (kHeadDim + 2) * sizeof(float), 256) : 256;
@@ -668,7 +668,7 @@ extern "C" DAPQ_API int dapq_paged_attention(const dapq_pages* pages, const dapq
   p.batch = pages->batch;
   p.total_new = (int32_t)step->total_new;
   p.each_new = (int32_t)(step->total_new / pages->batch);
-  p.max_new = step->max_new;
+  p.max_new = most_new(pages, step);
   p.n_q_heads = step->n_q_heads;
   p.parts = static_cast<float*>(workspace);
   p.group = step->n_q_heads / pages->n_kv_heads;
@@ -677,7 +677,7 @@ extern "C" DAPQ_API int dapq_paged_attention(const dapq_pages* pages, const dapq
   p.inv_items = 1.0f / (float)p.items;
   p.cap = step->softcap * kLog2e;
   p.c = step->softcap > 0.0f ? step->scale / step->softcap : step->scale * kLog2e;
-  const int64_t cols = (int64_t)step->max_new * p.group;
+  const int64_t cols = (int64_t)p.max_new * p.group;
   if (cols <= kMostRowCols) return launch_rows(pages, p, row_cols(cols), static_cast<hipStream_t>(stream));
   return launch_turn(pages, step, p, static_cast<hipStream_t>(stream));
 }

@@ -384,12 +384,11 @@ struct TurnPlan {
 };
 TurnPlan turn_plan(const dapq_pages* pages, const dapq_step* step) {
   const int64_t g = step->n_q_heads / pages->n_kv_heads;
-  const int64_t most = step->max_new < step->total_new ? step->max_new : step->total_new;  // tokens of a sequence
+  const int64_t most = most_new(pages, step);
   TurnPlan plan;
   const int64_t cols = kTurnCols, each = (most * g + cols - 1) / cols;
   const int64_t by_total = step->total_new * g / cols + pages->batch;
-  if (step->cu_new == nullptr) plan.blocks = pages->batch * (((step->total_new / pages->batch < most ? step->total_new / pages->batch : most) * g + cols - 1) / cols);
-  else plan.blocks = pages->batch * each < by_total ? pages->batch * each : by_total;
+  plan.blocks = step->cu_new == nullptr || pages->batch * each < by_total ? pages->batch * each : by_total;
   const int64_t groups = plan.blocks * pages->n_layers * pages->n_kv_heads;
   const int64_t tiles = ((int64_t)pages->max_pages * pages->page_rows + kTurnTile - 1) / kTurnTile;
   int64_t splits = groups > 0 ? 2048 / kTurnWaves / groups : 1;

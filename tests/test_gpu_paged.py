@@ -223,6 +223,18 @@ def test_attention_through_a_wide_table(fmt, case):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("page_rows", [16, 32, 64, 128, 256, 512, 1024])
+@pytest.mark.parametrize("new", [1, 30])
+def test_pages_of_all_sizes(fmt, page_rows, new):
+    rng = np.random.default_rng(page_rows)
+    rows = [1030 + new, 250 + new]
+    cache = Cache(rng, fmt, 1, 1, page_rows, rows).fill(rng, rows).to_device()
+    q = normal_bits(rng, 1, 2 * new, 2, 128)
+    got = check_attention(cache, [1030, 250], [new, new], q, ragged=False)
+    assert np.array_equal(attend(cache, [1030, 250], [new, new], q, max_new=1 << 30, ragged=False), got)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_a_long_sequence_among_many(fmt):
     """150 sequences, one of which has most of the rows, some none: parts of all lengths, also of sequences past the first 64."""
     rng = np.random.default_rng(301)

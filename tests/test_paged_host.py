@@ -171,6 +171,15 @@ def test_workspace_bytes_depend_on_no_device_data():
             assert n > 0 and n % 256 == 0
 
 
+def test_workspace_bytes_follow_the_tokens_that_there_can_be():
+    """max_new is a bound: without cu_new, and where it is more than all tokens, what is left of it counts."""
+    p = fp4(batch=4, max_pages=1000)
+    for cu in (N, A):
+        few, more = (D.paged_attention_workspace_bytes(p, step(total_new=4, max_new=m, cu_new=cu)) for m in (4 if cu else 1, 1 << 30))
+        assert few == more > 256
+    assert D.paged_attention_workspace_bytes(p, step(total_new=0, max_new=0)) > 0
+
+
 # --- the definition ---------------------------------------------------------------------------------------------------------
 def group(*values):
     x = np.zeros(128)
