@@ -359,8 +359,11 @@ int dapq_paged_read(const dapq_pages* pages, const int32_t* lengths, int32_t max
  *   out  device, bf16 [n_layers][total_new][n_q_heads][128], 16-byte aligned; 0 where no row is visible
  *   workspace  device scratch of at least dapq_paged_attention_workspace_bytes(pages, step), 256-byte aligned: sums of cache parts that
  *        were shared out.  The figure depends on neither the lengths nor cu_new, so that a recorded call holds for all of them.
- * Sums, maxima and weights are fp32, weights enter the product with the values as two bf16 numbers (16 bits of their
- * significand) for up to 32 query rows of a KV head (new tokens x H_q/H_kv) and as one beyond; the result is rounded once. */
+ * Sums, maxima and weights are fp32.  Weights enter the product with the values as two bf16 numbers (16 bits of their significand) where
+ * max_new x H_q/H_kv, the query rows of a KV head, is up to 32, and as one, rounded to nearest, beyond; the result is rounded once.
+ * A row that is infinite or no number reaches the queries that see it and no others.  How the rows are shared out over the chip follows the lengths;
+ * whether they are is decided by the table's width, max_pages x page_rows, so a table far wider than the lengths costs a short call a few microseconds.
+ */
 int dapq_paged_attention(const dapq_pages* pages, const dapq_step* step, const void* q, void* out, void* workspace,
                          size_t workspace_bytes, void* stream);
 
