@@ -99,19 +99,25 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
     for (int c = 0; c < 8; ++c) q[c] = *reinterpret_cast<const bf16x8*>(src + 16 * c + 8 * half);
   }
 
+  // (There before the loop: the waits in it would count them, and with them the rows that are on their way.)
+#pragma unroll
+  for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(q[c]));
+
   // Bringing in: this wave's rows of a tile, in registers, then in LDS.
   const int32_t* table = p.pool.table + (int64_t)seq * p.pool.max_pages;
   u32x4 kr[FP4 ? 1 : kTurnRows / 4], vr[FP4 ? 1 : kTurnRows / 4];
   unsigned ks = 0, vs = 0;
   int loaded_row = 0;  // the first of the rows in the registers
   bool loaded_page = false;
-  auto page_of = [&](int tile) {  // (one tile ahead of its rows)
-    const int64_t e = ((int64_t)tile * kTurnTile + kTurnRows * wave) >> p.pool.page_shift;
-    const int page = tile < tile1 && e < p.pool.max_pages ? table[e] : -1;
-    return page >= p.pool.n_pages ? -1 : page;
+  // A tile's entry of the table is read one tile ahead of its rows and looked at with them, since a wait for it is one for every load before it.
+  auto entry_of = [&](int tile) { return ((int64_t)tile * kTurnTile + kTurnRows * wave) >> p.pool.page_shift; };
+  auto page_of = [&](int tile) {
+    const int64_t e = entry_of(tile);
+    return table[e < p.pool.max_pages ? e : p.pool.max_pages - 1];
   };
   auto load_rows = [&](int tile, int page) {
     page = uniform(page);
+    page = tile < tile1 && entry_of(tile) < p.pool.max_pages && page < p.pool.n_pages ? page : -1;
     loaded_row = tile * kTurnTile + kTurnRows * wave;
     loaded_page = page >= 0;
     int rows = seen_by_last - loaded_row;
@@ -182,7 +188,7 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
     store_rows(0, tile0);
     load_rows(tile0 + 1, page_of(tile0 + 1));
   }
-  int page = page_of(tile0 + 2);
+  int page = tile0 < tile1 ? page_of(tile0 + 2) : -1;
   __syncthreads();
 
   for (int tile = tile0; tile < tile1; ++tile) {
