@@ -326,7 +326,8 @@ typedef struct dapq_step {
   int64_t v_stride_layer, v_stride_row, v_stride_head;
   int64_t q_stride_layer, q_stride_row, q_stride_head;
   float scale;            /* 1/sqrt(d_k) */
-  float softcap;          /* 0: none; > 0: a score x becomes softcap * tanh(x / softcap) */
+  float softcap;          /* 0: none; > 0: a score x becomes softcap * tanh(x / softcap); scale and softcap are up to 2^126, and
+                             scale / softcap is from 2^-110 to 2^110 */
 } dapq_step;
 
 /* Cache pruning into pages: dapq_gather with the cache in pages as its destination.  Row i < count of KV head h of sequence

@@ -257,6 +257,17 @@ def test_caps_of_all_sizes(softcap, new):
     check_attention(cache, [150], [new], normal_bits(rng, 1, new, 4, 128), softcap, scale=0.5)
 
 
+@pytest.mark.parametrize("softcap", [2.0 ** -100, 2.0 ** 108])
+@pytest.mark.parametrize("new", [1, 9])
+def test_caps_at_the_ends_of_their_range(softcap, new):
+    """Next to the smallest and the largest caps that are taken with this scale, also where a score is 0."""
+    rng = np.random.default_rng(72)
+    cache = Cache(rng, "bf16", 1, 1, 32, [150 + new]).fill(rng, [150 + new], gain=3.0).to_device()
+    q = normal_bits(rng, 1, new, 4, 128)
+    q[:, :, 1] = 0
+    check_attention(cache, [150], [new], q, softcap, scale=0.5)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("new", [[1, 1, 1, 1], [40, 3, 33, 20]])
 def test_attention_with_pages_missing(fmt, new):

@@ -142,6 +142,15 @@ def test_refusals(call, code, message):
     assert e.value.code == code
 
 
+@pytest.mark.parametrize("scale,softcap,message", [(2.0 ** 127, 0.0, "exceeds"), (1.0, 3e38, "exceeds"), (0.1, 1e36, "must be from"), (1.0, 1e-40, "must be from"),
+                                                   (2.0 ** -80, 2.0 ** 31, "must be from"), (2.0 ** 100, 2.0 ** -11, "must be from")])
+def test_scales_and_caps_without_a_usable_factor_are_refused(scale, softcap, message):
+    with pytest.raises(D.DapqError, match=message) as e:
+        attention(s=step(scale=scale, softcap=softcap))
+    assert e.value.code == ERR_UNSUPPORTED
+    assert D.paged_attention_workspace_bytes(pages(), step(scale=scale, softcap=softcap)) == 0
+
+
 def test_nothing_to_do_is_no_error():
     """No new tokens: nothing is enqueued (there is no GPU here), whatever the buffers."""
     for s in (step(total_new=0), step(max_new=0), step(total_new=0, cu_new=A)):
