@@ -291,7 +291,8 @@ int dapq_decode_attention(const dapq_shape* shape, const void* q_decode, const v
  *   DAPQ_PAGES_FP4   k, v: 128 codes at byte 64 * R, channel c in byte c / 2, the even channel in the low four bits;
  *                    k_scales, v_scales: 4 bytes at byte 4 * R, byte g for the channels 32g .. 32g + 31.  A code is a sign bit
  *                    (8) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; scale byte s multiplies it by 2^(s - 127), 255 makes all 32
- *                    NaN.  What the calls write are bf16 numbers, so nothing is rounded a second time when it is read.
+ *                    NaN.  What the calls write are finite bf16 numbers (s from 2 to 252) or NaN, so nothing is rounded a second time when
+ *                    it is read.  Pages may hold any s: at 253 the codes of 4 and 6 are past bf16 and count as infinite, at 254 those of 2 to 6.
  *                    What writes a group takes the least e in [-125, 125] with max |x| <= 7 * 2^e (at which 6 is still
  *                    a nearest level), rounds x / 2^e to the nearest level, of two the one with the even code, at most 6,
  *                    and writes s = e + 127; a group with an infinity or a NaN gets 255 (and codes 0).
@@ -362,6 +363,8 @@ int dapq_paged_read(const dapq_pages* pages, const int32_t* lengths, int32_t max
  *        were shared out.  The figure depends on neither the lengths nor cu_new, so that a recorded call holds for all of them.
  * Sums, maxima and weights are fp32.  Weights enter the product with the values as two bf16 numbers (16 bits of their significand) where
  * max_new x H_q/H_kv, the query rows of a KV head, is up to 32, and as one, rounded to nearest, beyond; the result is rounded once.
+ * A column's sum of weighted values is taken before it is divided by the weights', each of which is up to 2^4: it is infinite where 16 x rows x the largest value
+ * pass 2^128.
  * A row that is infinite or no number reaches the queries that see it and no others.  How the rows are shared out over the chip follows the lengths;
  * whether they are is decided by the table's width, max_pages x page_rows, so a table far wider than the lengths costs a short call a few microseconds.
  */

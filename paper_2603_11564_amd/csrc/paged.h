@@ -53,7 +53,7 @@ __device__ __forceinline__ unsigned fp4_scale_byte(unsigned largest) {
   const int kept = s < 2 ? 2 : (s > 252 ? 252 : s);
   return largest >= 0x7f80u ? kFp4Bad : (unsigned)kept;
 }
-// 2^(s - 127) as the conversions take it; s >= 2.
+// 2^(s - 127) as the conversions take it, which look at the exponent's bits alone: 0 counts as 2^-127, 255 as no number.
 __device__ __forceinline__ float fp4_scale(unsigned s) { return __uint_as_float(s << 23); }
 
 // Eight values (four dwords of two bf16) as codes.  bad: the group is not finite.
@@ -79,6 +79,12 @@ __device__ __forceinline__ unsigned fp4_unpack2(unsigned c, float s, int i) {
 // Eight codes as bf16 values.  A group without a scale (255) is NaN: the conversion makes its values so.
 __device__ __forceinline__ u32x4 fp4_unpack8(unsigned c, float s) {
   return u32x4{fp4_unpack2(c, s, 0), fp4_unpack2(c, s, 1), fp4_unpack2(c, s, 2), fp4_unpack2(c, s, 3)};
+}
+
+// Eight codes of which those are 0 whose values with the scale s are no finite bf16: all of them without a scale, 2 and more at 2^127, 4 and 6 at 2^126.
+__device__ __forceinline__ unsigned fp4_finite8(unsigned c, float s) {
+  const unsigned past = s > 0x1p127f ? ~0u : (s > 0x1p126f ? c >> 2 : (s > kLargestFp4Scale ? c >> 2 & c >> 1 : 0u));  // (in the lowest bit of each code)
+  return c & ~((past & 0x11111111u) * 15u);
 }
 
 // The larger of the two magnitudes in a dword.

@@ -328,17 +328,17 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
         // Rows that no column sees may hold anything, and 0 times it must be 0.  A value that is infinite or no number, in a row that some columns
         // see and others don't, is added to the former by itself, in LDS.
         bool odd = false;
+        float top = 0.0f;  // FP4: the largest scale of such rows
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int row = row0 + 16 * (e >> 2) + 4 * kg + (e & 3);
           const bool none = row >= seen_by_last || !now.ok[e >> 2];
           if constexpr (FP4) {
-            const bool bad = vscale[e] > kLargestFp4Scale || vscale[e] != vscale[e];
-            odd |= bad && !none && row >= seen_by_all;
-            if (none || (bad && row >= seen_by_all)) {
+            if (none) {
               b.vc[e] = 0;
               vscale[e] = 1.0f;
             }
+            top = fmaxf(top, row >= seen_by_all ? vscale[e] : 0.0f);
           } else {
             if (none) b.vt[e] = u32x4{0, 0, 0, 0};
             if (row >= seen_by_all) {
@@ -351,7 +351,15 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
             }
           }
         }
-        if (__any(odd)) {
+        if (__any(odd || top > kLargestFp4Scale)) {
+          if constexpr (FP4) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (row0 + 16 * (e >> 2) + 4 * kg + (e & 3) < seen_by_all) continue;
+              b.vc[e] = fp4_finite8(b.vc[e], vscale[e]);
+              if (vscale[e] > 0x1p127f) vscale[e] = 1.0f;  // (0 without a scale is no number)
+            }
+          }
           if (!apart) {
             for (int i = lane; i < kCols * kHeadDim; i += 64) mine[i] = 0.0f;
             apart = true;

@@ -144,10 +144,11 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
     if constexpr (FP4) {
       const int row = kTurnRows * wave + (lane >> 2);
       float scale = fp4_scale(vs);
-      if (loaded_row + (lane >> 2) >= seen_by_all && (scale > kLargestFp4Scale || scale != scale)) {
+      if (loaded_row + (lane >> 2) >= seen_by_all && scale > kLargestFp4Scale) {
         odd = true;
-        scale = 1.0f;
-        vr[0] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vr[0][i] = fp4_finite8(vr[0][i], scale);
+        if (scale > 0x1p127f) scale = 1.0f;  // (0 without a scale is no number)
       }
       if (lane >> 2 < kTurnRows)
 #pragma unroll
