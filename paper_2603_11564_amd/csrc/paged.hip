@@ -20,10 +20,10 @@ int check_pages(const dapq_pages* p) {
                "page_rows (%d) must be a power of two from 16 to 1024", p->page_rows);
   DAPQ_REQUIRE((int64_t)p->max_pages * p->page_rows < (int64_t)1 << 30, DAPQ_ERR_UNSUPPORTED,
                "max_pages (%d) * page_rows (%d) must be below 2^30", p->max_pages, p->page_rows);
-  DAPQ_REQUIRE((int64_t)p->n_layers * p->batch * p->n_kv_heads < (int64_t)1 << 24, DAPQ_ERR_UNSUPPORTED,
-               "n_layers * batch * n_kv_heads (%lld) of the pages must be below 2^24", (long long)p->n_layers * p->batch * p->n_kv_heads);
   DAPQ_REQUIRE((int64_t)p->n_layers * p->n_kv_heads <= 65535, DAPQ_ERR_UNSUPPORTED, "n_layers * n_kv_heads (%lld) of the pages exceeds 65535",
                (long long)p->n_layers * p->n_kv_heads);
+  DAPQ_REQUIRE((int64_t)p->n_layers * p->batch * p->n_kv_heads < (int64_t)1 << 24, DAPQ_ERR_UNSUPPORTED,
+               "n_layers * batch * n_kv_heads (%lld) of the pages must be below 2^24", (long long)p->n_layers * p->batch * p->n_kv_heads);
   DAPQ_REQUIRE((int64_t)p->n_pages * p->page_rows / 16 <= ((int64_t)0xfffffff0 / ((int64_t)p->n_layers * p->n_kv_heads)), DAPQ_ERR_UNSUPPORTED,
                "n_pages (%d) of page_rows (%d) are more than 2^36 rows of all layers and heads", p->n_pages, p->page_rows);
   DAPQ_REQUIRE(p->k != nullptr && p->v != nullptr && p->table != nullptr, DAPQ_ERR_INVALID_ARG, "k, v and table of the pages must not be NULL");
