@@ -58,6 +58,21 @@ def test_appends_of_many_tokens(fmt, layers, heads, lengths, new, pairing):
     same_pool(cache.from_device(), cache.pool)
 
 
+@pytest.mark.parametrize("heads", [65534, 65535])
+def test_an_append_of_the_most_heads(heads):
+    """One token: 32767 and 32768 pairs of heads of the keys and as many of the values, along one axis of a launch, which holds 65536."""
+    g = torch.Generator(device="cuda").manual_seed(heads)
+    new = [torch.empty((1, 1, heads, 128), dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(2)]
+    pools = [torch.zeros((1, 2, heads, 16, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    pages = D.make_pages(n_layers=1, batch=1, n_kv_heads=heads, page_rows=16, n_pages=2, max_pages=1, format="bf16", k=pools[0], v=pools[1], table=dev_int([1]))
+    strides = (heads * 128, heads * 128, 128)
+    D.dapq_paged_append(pages, make_step([3], [1], False, heads, k_strides=strides, v_strides=strides), *new, None, THETA)
+    for pool, x in zip(pools, new):
+        assert torch.equal(pool[0, 1, :, 3], x[0, 0])
+        pool[0, 1, :, 3] = 0
+        assert not pool.any()
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("layers,heads,lens,budget,page_rows,layout", [
     (2, 4, [50, 90], 900, 16, "thd"),       # a budget of 8 MB and more: stores past the caches
