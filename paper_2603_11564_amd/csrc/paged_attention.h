@@ -27,7 +27,10 @@ inline int32_t most_new(const dapq_pages* pages, const dapq_step* step) {
   return (int32_t)(step->max_new < n ? step->max_new : n);
 }
 
-// The call with more columns (new tokens x query heads of a KV head) than the row kernel takes.
+// The columns (new tokens x query heads of a KV head) that the row kernel takes, two blocks of 16: it reads a row in place, where the turn kernel passes it through
+// LDS and has 128 columns to a workgroup, used or not.  Us, row / turn kernel, 8 KV heads, 32 columns: 1 sequence of 1000 rows 14.8 / 14.1, of 100000 84.6 / 96.2, 32 of 4000
+// 108.5 / 106.3, 64 of 1000 54.3 / 52.6; in 4 bits 16.3 / 14.6, 40.3 / 72.8, 45.4 / 74.0, 24.4 / 35.8.  4 columns: 11.8 / 13.4, 82.9 / 94.7, 97.9 / 100.6, 48.4 / 50.9; in 4 bits
+// 9.2 / 14.1, 31.3 / 70.6, 36.4 / 69.6, 14.6 / 34.4.
 constexpr int kMostRowCols = 32;
 size_t turn_workspace_bytes(const dapq_pages* pages, const dapq_step* step);
 int launch_turn(const dapq_pages* pages, const dapq_step* step, const PagedAttentionParams& p, hipStream_t stream);

@@ -14,7 +14,7 @@ constexpr int kTurnTile = 64;   // cache rows of a tile
 constexpr int kTurnWaves = 4;
 constexpr int kTurnTileBytes = kTurnTile * kRowBytes;  // of K or V in LDS, as bf16
 constexpr int kTurnCols = 32 * kTurnWaves;   // of a workgroup
-constexpr int kTurnRows = kTurnTile / kTurnWaves;  // that a wave brings in: 8 or 16, which are on one page
+constexpr int kTurnRows = kTurnTile / kTurnWaves;  // that a wave brings in: 16, which are on one page
 
 struct TurnParams : PagedAttentionParams {
   int32_t blocks, splits;  // blocks of columns of all sequences, at most; parts of the rows
@@ -150,7 +150,6 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
         for (int i = 0; i < 4; ++i) vr[0][i] = fp4_finite8(vr[0][i], scale);
         if (scale > 0x1p127f) scale = 1.0f;  // (0 without a scale is no number)
       }
-      if (lane >> 2 < kTurnRows)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         *reinterpret_cast<u32x4*>(kt + chunk_at(row, 4 * (lane & 3) + i)) = fp4_unpack8(kr[0][i], fp4_scale(ks));
@@ -402,6 +401,11 @@ TurnPlan turn_plan(const dapq_pages* pages, const dapq_step* step) {
   plan.blocks = step->cu_new == nullptr || pages->batch * each < by_total ? pages->batch * each : by_total;
   const int64_t groups = plan.blocks * pages->n_layers * pages->n_kv_heads;
   const int64_t tiles = ((int64_t)pages->max_pages * pages->page_rows + kTurnTile - 1) / kTurnTile;
+  // Parts for the 512 workgroups that the chip holds, of four tiles or more.  Us, one part / for 256 workgroups / 512 / 1024, 4 query heads of 8 KV heads, bf16:
+  // 16 tokens behind 1000 rows 30 / 15 / 15 / 15, behind 100000 2290 / 97 / 100 / 132, of 8 sequences of 4000 rows 102 / 40 / 41 / 52, of 32 of them 106 / 107 / 114 / 124,
+  // 500 tokens behind 1000 rows 48 / 39 / 36 / 45, 300 behind 8000 218 / 89 / 70 / 82; in 4 bits 16 tokens behind 100000 rows 2321 / 94 / 80 / 105, of 32 sequences of
+  // 4000 rows 103 / 104 / 85 / 92.  Parts of two tiles or more / four / eight: 16 tokens behind 1000 rows 12.8 / 15.1 / 21.1, behind 4000 24.0 / 22.2 / 25.5, of 8 sequences
+  // of 1000 rows 22.3 / 19.9 / 24.0, 500 tokens behind 1000 36.1 / 36.2 / 39.4.
   int64_t splits = groups > 0 ? 2048 / kTurnWaves / groups : 1;
   if (splits > tiles / 4) splits = tiles / 4;
   plan.splits = (int)(splits < 1 ? 1 : splits);
