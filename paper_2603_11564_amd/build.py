@@ -39,7 +39,7 @@ def _hipcc() -> str:
 
 
 # Host-side sanitizers for the library's host code (argument checks, launch plans, workspace carving); the device
-# code is compiled as usual.  Used by tests/test_host_sanitizers.py, which runs the host boundary tests against it.
+# code is compiled as usual.  Used by tests/test_host_sanitizers.py and tests/test_paged_sanitizers.py, which run the host tests against it.
 SANITIZE_FLAGS = ["-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
                   "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host", "-fno-omit-frame-pointer"]
 SANITIZED_LIB = os.path.join(PKG, "_build", "san", "libdapq_san.so")

@@ -78,8 +78,10 @@ struct Part {
 //   logits   D[row][column] = K (A operand, 16 rows x 32 channels) x q (B operand); a lane has four rows of one column.
 //   weights  2^(c * logit - ref) in fp32; ref only moves, and the sums are rescaled, where a logit lies more than kHeadroom binades above it.
 //   output   D[column][channel] += weights (A) x V (B); a weight enters as two bf16 numbers, the leading 8 bits of its significand and the next 8.
+//            What is cut off is less than 2^-15 of a weight and 2^-17 on average, always downwards, while the sum below the fraction has all 24 bits: 2^-9 of half a
+//            step of the result.  A third number would be another product for every eight channels where columns exceed 8.
 //            V is transposed in registers: a lane loads the same 8 channels of 8 rows.
-// Bound by bytes where there are enough items: bf16, 256 sequences of 1000 rows, 8 KV heads 182 us (5.8 TB/s), in 4 bits 55 (5.1 TB/s, where 342 vector
+// Bound by bytes where there are enough items: bf16, 256 sequences of 1000 rows, 8 KV heads 182 us (5.8 TB/s), in 4 bits 55 (5.1 TB/s, where 335 vector
 // instructions a tile begin to count: three waves to a SIMD, two take 63); one item alone takes 0.27 us a tile in bf16, 0.16 in 4 bits, behind 5 to 6 us.
 // BLOCKS: blocks of 16 columns; 0: up to 8 columns, whose leading and following parts take the two halves of one block.
 // SPLIT: a workgroup has a part of an item; else an item (and nothing is to be joined).
