@@ -363,13 +363,13 @@ int dapq_paged_read(const dapq_pages* pages, const int32_t* lengths, int32_t max
  *        were shared out.  The figure depends on neither the lengths nor cu_new, so that a recorded call holds for all of them.
  * Sums, maxima and weights are fp32.  Weights enter the product with the values as two bf16 numbers (the leading 16 bits of their significand, the others cut off) where
  * max_new x H_q/H_kv, the query rows of a KV head, is up to 32, and as one, rounded to nearest, beyond; the result is rounded once.
- * A column's sum of weighted values is taken before it is divided by the weights', each of which is up to 2^4: it is infinite where 16 x rows x the largest value
- * pass 2^128.
+ * A column's sum of weighted values is taken before it is divided by the weights', each of which is up to 2^4: it may be infinite where 16 x rows x the largest
+ * value pass 2^128.
  * A row that is infinite or no number reaches the queries that see it and no others.  How the rows are shared out over the chip follows the lengths; whether they are is
  * decided by the table's width, max_pages x page_rows: through a table of 131072 rows a step of 64 sequences of 256..1100 takes 45 us for 38 through one as wide as the
  * longest, in 4 bits 21 for 15.
- * The kernel is that of the bound, max_new: a long turn and single tokens behind long caches cost less in two calls (500 tokens and 63 sequences with one over 4000 rows 206 us
- * in one call, 36 and 179 in two; 2500 tokens and 7 with one over 100000 rows 2400, 126 and 479).
+ * The kernel is that of the bound, max_new, so that a long turn and single tokens behind long caches can cost less in two calls (2500 tokens and 7 sequences with one over
+ * 100000 rows 2400 us in one call, 126 and 479 in two; 500 tokens and 63 with one over 4000 rows in 4 bits 166, 36 and 51, in bf16 206, 36 and 179).
  */
 int dapq_paged_attention(const dapq_pages* pages, const dapq_step* step, const void* q, void* out, void* workspace,
                          size_t workspace_bytes, void* stream);
