@@ -279,7 +279,7 @@ int dapq_decode_attention(const dapq_shape* shape, const void* q_decode, const v
 
 /* --- Decoding over a cache in pages ------------------------------------------------------------------------------
  * dapq_gather and dapq_decode_attention work on a compact cache of a fixed number of rows.  The calls below hold a
- * sequence's rows in pages of a pool instead, as bf16 or in 4 bits: the rows that the eviction kept come first
+ * sequence's rows in pages of a pool instead, as bf16, in 8 or in 4 bits: the rows that the eviction kept come first
  * (dapq_paged_gather), the rows of the tokens that are decoded, or of the conversation's next turn, follow
  * (dapq_paged_append), and dapq_paged_attention reads them.  A row's place in the cache and its position are two
  * things here: behind an eviction that kept 983 rows of 32768, row 983 stands for position 32768.
@@ -296,9 +296,16 @@ int dapq_decode_attention(const dapq_shape* shape, const void* q_decode, const v
  *                    What writes a group takes the least e in [-125, 125] with max |x| <= 7 * 2^e (at which 6 is still
  *                    a nearest level), rounds x / 2^e to the nearest level, of two the one with the even code, at most 6,
  *                    and writes s = e + 127; a group with an infinity or a NaN gets 255 (and codes 0).
+ *   DAPQ_PAGES_E4M3  k, v: 128 codes at byte 128 * R, channel c in byte c; k_scales, v_scales: as FP4's.  A code is a sign bit (128), four exponent bits E and
+ *                    three bits M: (8 + M) * 2^(E - 10), M * 2^-9 where E is 0, no number where all seven are set; scale byte s multiplies it by
+ *                    2^(s - 127), 255 makes all 32 NaN.  What the calls write are finite bf16 numbers (s from 10 to 246), none of them subnormal, or NaN groups.
+ *                    Pages may hold any s and the code without a number: values past bf16 (448 at 247, 2 and more at 254) count as infinite.
+ *                    What writes a group takes the least e in [-117, 119] with max |x| <= 464 * 2^e (at which 448 is still a nearest level),
+ *                    rounds x / 2^e to the nearest level, of two the one with the even code, at most 448, and writes s = e + 127; a
+ *                    group with an infinity or a NaN gets 255 (and codes 0).
  * An entry of the table outside [0, n_pages) is no page, and rows past max_pages * page_rows are on no page: nothing is written
  * there, and nothing read.  Two sequences may share pages that neither call writes to. */
-enum { DAPQ_PAGES_BF16 = 0, DAPQ_PAGES_FP4 = 1 };
+enum { DAPQ_PAGES_BF16 = 0, DAPQ_PAGES_FP4 = 1, DAPQ_PAGES_E4M3 = 3 }; /* (2 is none) */
 typedef struct dapq_pages {
   int32_t n_layers;
   int32_t batch;          /* sequences of the table; dapq_paged_gather and dapq_paged_read take up to 65535 */
@@ -332,15 +339,15 @@ typedef struct dapq_step {
 } dapq_step;
 
 /* Cache pruning into pages: dapq_gather with the cache in pages as its destination.  Row i < count of KV head h of sequence
- * seq becomes the prompt's row idx[i] of that head; FP4 pages quantise it.  shape, k, v, idx, count and budget are those of
+ * seq becomes the prompt's row idx[i] of that head; FP4 and E4M3 pages quantise it.  shape, k, v, idx, count and budget are those of
  * dapq_gather; the layers, the batch and the KV heads of shape and pages must be the same.  Rows past count, and rows whose index lies
  * outside the prompt, are left as they were.  k and v must not overlap the pages. */
 int dapq_paged_gather(const dapq_shape* shape, const dapq_pages* pages, const void* k, const void* v, const int32_t* idx,
                       const int32_t* count, int32_t budget, void* stream);
 
 /* The rows of new tokens go behind what each sequence holds: row lengths[seq] + t becomes
- *   K: RoPE_{positions[cu_new[seq] + t]}(k_new), rounded to bf16 once as by dapq_rope_apply (FP4 pages: then quantised)
- *   V: v_new (FP4 pages: quantised)
+ *   K: RoPE_{positions[cu_new[seq] + t]}(k_new), rounded to bf16 once as by dapq_rope_apply (FP4, E4M3: then quantised)
+ *   V: v_new (FP4, E4M3: quantised)
  *   k_new, v_new  device, bf16, element (layer, token, head, c) at layer*stride_layer + token*stride_row + head*stride_head + c
  *   positions     device, int32 [total_new], >= 0; NULL: the keys are stored as they are (theta, pairing unused)
  * Uses cu_new, lengths, max_new, total_new and the K and V strides of step.  Two sequences must not append to one page. */

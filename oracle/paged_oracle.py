@@ -1,8 +1,8 @@
-"""Float64 CPU definition of the cache in pages: the FP4 rows, writing and reading rows, attention over them.
+"""Float64 CPU definition of the cache in pages: the FP4 and E4M3 rows, writing and reading rows, attention over them.
 
 TEST INFRASTRUCTURE ONLY, as dapq_oracle.  A pool is a dict of numpy arrays as they lie in memory: "k" and "v" are bf16
-bits uint16 [layers][n_pages][heads][page_rows][128], or codes uint8 [...][64] with "k_scales", "v_scales" uint8
-[...][4].  Every function changes copies.
+bits uint16 [layers][n_pages][heads][page_rows][128], or codes uint8 [...][64] (FP4) or [...][128] (E4M3) with "k_scales",
+"v_scales" uint8 [...][4].  Every function changes copies.
 """
 from __future__ import annotations
 
@@ -44,6 +44,43 @@ def fp4_values(codes, scales):
     return np.where(c >= 8, -1.0, 1.0) * LEVELS[c & 7] * np.repeat(two, 32, -1)
 
 
+# Magnitudes of the E4M3 codes 0 .. 126: E = 0 counts as E = 1 without the leading 8.  127 is no number.
+E4M3_LEVELS = np.array([(m if e == 0 else 8 + m) * 2.0 ** (max(e, 1) - 10) for e in range(16) for m in range(8)][:127])
+
+
+def e4m3_quantise(x):
+    """Float64 rows [..., 128] -> codes uint8 [..., 128], scale bytes uint8 [..., 4].
+
+    Per group of 32 channels the least e in [-117, 119] with max |x| <= 464 * 2^e; each value the level nearest to x / 2^e, of
+    two the one with the even code, at most 448.  Groups that are not finite: scale byte 255, codes 0."""
+    x = np.asarray(x, dtype=np.float64)
+    g = x.reshape(x.shape[:-1] + (4, 32))
+    bad = ~np.isfinite(g).all(-1)
+    g0 = np.where(bad[..., None], 0.0, g)
+    largest = np.abs(g0).max(-1)
+    e = np.full(largest.shape, -117)
+    for candidate in range(-116, 120):
+        e = np.where(largest > 464.0 * 2.0 ** (candidate - 1), candidate, e)
+    y = np.abs(g0) / (2.0 ** e)[..., None]
+    distance = np.abs(y[..., None] - E4M3_LEVELS)
+    nearest = distance == distance.min(-1, keepdims=True)
+    prefer = 1 - np.arange(127) % 2                             # of two nearest levels the even code
+    code = np.argmax(nearest * (1 + prefer), -1) + np.where(np.signbit(g0), 128, 0)
+    return np.where(bad[..., None], 0, code).reshape(x.shape).astype(np.uint8), np.where(bad, 255, e + 127).astype(np.uint8)
+
+
+def e4m3_values(codes, scales):
+    """The values that codes and scale bytes stand for, float64 [..., 128]."""
+    c = np.asarray(codes).astype(np.int64)
+    two = np.where(np.asarray(scales) == 255, np.nan, 2.0 ** (np.asarray(scales).astype(np.float64) - 127.0))
+    return np.where(c >= 128, -1.0, 1.0) * np.append(E4M3_LEVELS, np.nan)[c & 127] * np.repeat(two, 32, -1)
+
+
+def code_values(codes, scales):
+    """Of the format whose rows have as many bytes."""
+    return (fp4_values if np.asarray(codes).shape[-1] == 64 else e4m3_values)(codes, scales)
+
+
 def place(table, n_pages, page_rows, seq, i):
     """(page, slot) of row i of a sequence, or None if it is on no page."""
     if i < 0 or i >= table.shape[1] * page_rows:
@@ -56,7 +93,8 @@ def put(pool, name, layer, head, where, bits):
     """One bf16 row (bits [128]) into the pool, in place."""
     page, slot = where
     if name + "_scales" in pool:
-        codes, scales = fp4_quantise(bf16_bits_to_f64(bits))
+        quantise = fp4_quantise if pool[name].shape[-1] == 64 else e4m3_quantise
+        codes, scales = quantise(bf16_bits_to_f64(bits))
         pool[name][layer, page, head, slot] = codes
         pool[name + "_scales"][layer, page, head, slot] = scales
     else:
@@ -67,7 +105,7 @@ def value(pool, name, layer, head, where):
     """One row of the pool, float64 [128]."""
     page, slot = where
     row = pool[name][layer, page, head, slot]
-    return fp4_values(row, pool[name + "_scales"][layer, page, head, slot]) if name + "_scales" in pool else bf16_bits_to_f64(row)
+    return code_values(row, pool[name + "_scales"][layer, page, head, slot]) if name + "_scales" in pool else bf16_bits_to_f64(row)
 
 
 def _shape(pool):
@@ -140,7 +178,7 @@ def attention(pool, table, lengths, cu_new, q, scale, softcap=0.0):
                 if not rows or not new:
                     continue
                 pages, slots = table[seq, at // page_rows], at % page_rows
-                k, v = (fp4_values(pool[n][layer, pages, head, slots], pool[n + "_scales"][layer, pages, head, slots])
+                k, v = (code_values(pool[n][layer, pages, head, slots], pool[n + "_scales"][layer, pages, head, slots])
                         if n + "_scales" in pool else bf16_bits_to_f64(pool[n][layer, pages, head, slots]) for n in ("k", "v"))
                 for t in range(new):
                     r, seen = int(cu_new[seq]) + t, at <= int(lengths[seq]) + t

@@ -315,12 +315,12 @@ def dapq_pseudo_queries(desc, x, token_idx, w_q, positions, theta, pairing, q_ou
         _check(rc)
 
 
-PAGE_FORMATS = {"bf16": 0, "fp4": 1}
+PAGE_FORMATS = {"bf16": 0, "fp4": 1, "e4m3": 3}
 
 
 def make_pages(*, n_layers, batch, n_kv_heads, page_rows, n_pages, max_pages, format, k, v, table, k_scales=None, v_scales=None,
                head_dim=128) -> Pages:
-    """format: "bf16" or "fp4".  k, v, k_scales, v_scales: the pools; table: device int32 [batch][max_pages].  The descriptor keeps them alive."""
+    """format: "bf16", "fp4" or "e4m3".  k, v, k_scales, v_scales: the pools; table: device int32 [batch][max_pages].  The descriptor keeps them alive."""
     p = Pages()
     p.n_layers, p.batch, p.n_kv_heads, p.head_dim = n_layers, batch, n_kv_heads, head_dim
     p.format, p.page_rows, p.n_pages, p.max_pages = PAGE_FORMATS[format], page_rows, n_pages, max_pages

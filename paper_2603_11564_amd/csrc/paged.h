@@ -1,4 +1,4 @@
-// The page pool as the kernels see it, and the FP4 rows of it.
+// The page pool as the kernels see it, and the FP4 and E4M3 rows of it.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -25,12 +25,23 @@ inline PagePool page_pool(const dapq_pages* p) {
 namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
+// Formats, as the kernels' template arguments.
+constexpr int kBf16 = DAPQ_PAGES_BF16, kFp4 = DAPQ_PAGES_FP4, kE4m3 = DAPQ_PAGES_E4M3;
 constexpr int kRowBytes = 2 * kHeadDim;      // of a bf16 row
-constexpr int kFp4RowBytes = kHeadDim / 2;   // the codes of an FP4 row; and 4 scale bytes
-constexpr float kLargestFp4Scale = 0x1p125f;  // of finite values: 6 * 2^125 is a bf16, 6 * 2^126 is not
-constexpr unsigned kFp4Bad = 255;            // scale byte of a group with a value that is not finite
+template <int FMT>
+constexpr int kCodeBytes = FMT == kBf16 ? kRowBytes : (FMT == kFp4 ? kHeadDim / 2 : kHeadDim);  // of a row; codes have 4 scale bytes beside them
+template <int FMT>
+constexpr float kLargestScale = FMT == kFp4 ? 0x1p125f : 0x1p119f;  // of finite values: 6 * 2^125 and 448 * 2^119 are bf16 numbers, twice as much is not
+constexpr unsigned kNoScale = 255;           // scale byte of a group with a value that is not finite
+// Bytes of a row with its scales (host).
+inline int row_bytes(const dapq_pages* p) {
+  return p->format == DAPQ_PAGES_BF16 ? kRowBytes : (p->format == DAPQ_PAGES_FP4 ? kCodeBytes<kFp4> : kCodeBytes<kE4m3>) + 4;
+}
 
 // Row number of slot 0 of a page of one head.
 __device__ __forceinline__ int64_t page_row(const PagePool& p, int layer, int page, int head) {
@@ -51,21 +62,32 @@ __device__ __forceinline__ int64_t find_row(const PagePool& p, int layer, int64_
 __device__ __forceinline__ unsigned fp4_scale_byte(unsigned largest) {
   const int s = (int)((largest + (127 - 96)) >> 7) - 2;  // (the sum carries into the exponent from m = 97 on)
   const int kept = s < 2 ? 2 : (s > 252 ? 252 : s);
-  return largest >= 0x7f80u ? kFp4Bad : (unsigned)kept;
+  return largest >= 0x7f80u ? kNoScale : (unsigned)kept;
+}
+// The same of E4M3: the least e in [-117, 119] with max <= 464 * 2^e.  464 = (1 + 104 / 128) * 2^8: e is x - 8, or x - 7 if m > 104.  2^-9, the least
+// code's value, is then a normal bf16 number at every scale.
+__device__ __forceinline__ unsigned e4m3_scale_byte(unsigned largest) {
+  const int s = (int)((largest + (127 - 104)) >> 7) - 8;
+  const int kept = s < 10 ? 10 : (s > 246 ? 246 : s);
+  return largest >= 0x7f80u ? kNoScale : (unsigned)kept;
+}
+template <int FMT>
+__device__ __forceinline__ unsigned scale_byte_of(unsigned largest) {
+  return FMT == kFp4 ? fp4_scale_byte(largest) : e4m3_scale_byte(largest);
 }
 // 2^(s - 127) as the conversions take it, which look at the exponent's bits alone: 0 counts as 2^-127, 255 as no number.
-__device__ __forceinline__ float fp4_scale(unsigned s) { return __uint_as_float(s << 23); }
+__device__ __forceinline__ float group_scale(unsigned s) { return __uint_as_float(s << 23); }
 
 // Eight values (four dwords of two bf16) as codes.  bad: the group is not finite.
 __device__ __forceinline__ unsigned fp4_pack8(u32x4 x, unsigned scale_byte) {
-  const float s = fp4_scale(scale_byte);
+  const float s = group_scale(scale_byte);
   const unsigned x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];  // (a bit_cast of a vector's element takes its first)
   unsigned c = 0;
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, x0), s, 0);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, x1), s, 1);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, x2), s, 2);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, x3), s, 3);
-  return scale_byte == kFp4Bad ? 0u : c;
+  return scale_byte == kNoScale ? 0u : c;
 }
 // Codes 2i and 2i + 1 of eight.
 __device__ __forceinline__ unsigned fp4_unpack2(unsigned c, float s, int i) {
@@ -81,11 +103,44 @@ __device__ __forceinline__ u32x4 fp4_unpack8(unsigned c, float s) {
   return u32x4{fp4_unpack2(c, s, 0), fp4_unpack2(c, s, 1), fp4_unpack2(c, s, 2), fp4_unpack2(c, s, 3)};
 }
 
-// Eight codes of which those are 0 whose values with the scale s are no finite bf16: all of them without a scale, 2 and more at 2^127, 4 and 6 at 2^126.
+// Eight codes of FP4 of which those are 0 whose values with the scale s are no finite bf16: all of them without a scale, 2 and more at 2^127, 4 and 6 at 2^126.
 __device__ __forceinline__ unsigned fp4_finite8(unsigned c, float s) {
-  const unsigned past = s > 0x1p127f ? ~0u : (s > 0x1p126f ? c >> 2 : (s > kLargestFp4Scale ? c >> 2 & c >> 1 : 0u));  // (in the lowest bit of each code)
+  const unsigned past = s > 0x1p127f ? ~0u : (s > 0x1p126f ? c >> 2 : (s > kLargestScale<kFp4> ? c >> 2 & c >> 1 : 0u));  // (in the lowest bit of each code)
   return c & ~((past & 0x11111111u) * 15u);
 }
+
+// Two values as E4M3 codes, in the low half.  The conversion rounds to nearest, ties to even, and makes what is past the levels no number: only at the
+// largest scale there may be such values, which become 448.
+__device__ __forceinline__ unsigned e4m3_pack2(unsigned x, unsigned scale_byte) {
+  if (scale_byte == 246u) {
+    const unsigned most = 0x7f607f60u;  // 448 * 2^119
+    const unsigned m = __builtin_bit_cast(unsigned, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x & 0x7fff7fffu), __builtin_bit_cast(u16x2, most)));
+    x = m | (x & 0x80008000u);
+  }
+  const s16x2 c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, __builtin_bit_cast(bf16x2, x), group_scale(scale_byte), 0);
+  return scale_byte == kNoScale ? 0u : __builtin_bit_cast(unsigned, c) & 0xffffu;
+}
+__device__ __forceinline__ u32x2 e4m3_pack8(u32x4 x, unsigned scale_byte) {
+  const unsigned x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];
+  return u32x2{e4m3_pack2(x0, scale_byte) | e4m3_pack2(x1, scale_byte) << 16, e4m3_pack2(x2, scale_byte) | e4m3_pack2(x3, scale_byte) << 16};
+}
+// Codes 2i and 2i + 1 of four.  The code 127 is no number, and neither is any code of a group without a scale.
+__device__ __forceinline__ unsigned e4m3_unpack2(unsigned c, float s, int i) {
+  return i == 0 ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, 0))
+                : __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, 1));
+}
+__device__ __forceinline__ u32x4 e4m3_unpack8(unsigned c0, unsigned c1, float s) {
+  return u32x4{e4m3_unpack2(c0, s, 0), e4m3_unpack2(c0, s, 1), e4m3_unpack2(c1, s, 0), e4m3_unpack2(c1, s, 1)};
+}
+
+// The highest bits of those of four E4M3 codes whose values with the scale s are no finite bf16: 127 at any scale, from 2^8 on (0x78) at 2^120, from 2^7
+// on (0x70) at 2^121, ..., all of them without a scale.
+__device__ __forceinline__ unsigned e4m3_past(unsigned c, float s) {
+  const int over = (int)(__float_as_uint(s) >> 23) - (119 + 127);
+  const unsigned to_bit = over <= 0 ? 1u : (over >= 9 ? 0x80u : 8u * over);  // takes the first such code to 128
+  return ((c & 0x7f7f7f7fu) + to_bit * 0x01010101u) & 0x80808080u;
+}
+__device__ __forceinline__ unsigned e4m3_finite4(unsigned c, float s) { return c & ~((e4m3_past(c, s) >> 7) * 255u); }
 
 // The larger of the two magnitudes in a dword.
 __device__ __forceinline__ unsigned larger_magnitude(unsigned x) {

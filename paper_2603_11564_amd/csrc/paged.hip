@@ -14,7 +14,7 @@ int check_pages(const dapq_pages* p) {
                "n_layers (%d), batch (%d), n_kv_heads (%d), n_pages (%d) and max_pages (%d) of the pages must be >= 1", p->n_layers,
                p->batch, p->n_kv_heads, p->n_pages, p->max_pages);
   DAPQ_REQUIRE(p->head_dim == kHeadDim, DAPQ_ERR_UNSUPPORTED, "head_dim %d is not supported (128 only)", p->head_dim);
-  DAPQ_REQUIRE(p->format == DAPQ_PAGES_BF16 || p->format == DAPQ_PAGES_FP4, DAPQ_ERR_INVALID_ARG, "format (%d) is none of DAPQ_PAGES_*",
+  DAPQ_REQUIRE(p->format == DAPQ_PAGES_BF16 || p->format == DAPQ_PAGES_FP4 || p->format == DAPQ_PAGES_E4M3, DAPQ_ERR_INVALID_ARG, "format (%d) is none of DAPQ_PAGES_*",
                p->format);
   DAPQ_REQUIRE(p->page_rows >= 16 && p->page_rows <= 1024 && (p->page_rows & (p->page_rows - 1)) == 0, DAPQ_ERR_UNSUPPORTED,
                "page_rows (%d) must be a power of two from 16 to 1024", p->page_rows);
@@ -28,8 +28,9 @@ int check_pages(const dapq_pages* p) {
                "n_pages (%d) of page_rows (%d) are more than 2^36 rows of all layers and heads", p->n_pages, p->page_rows);
   DAPQ_REQUIRE(p->k != nullptr && p->v != nullptr && p->table != nullptr, DAPQ_ERR_INVALID_ARG, "k, v and table of the pages must not be NULL");
   uintptr_t bits = reinterpret_cast<uintptr_t>(p->k) | reinterpret_cast<uintptr_t>(p->v);
-  if (p->format == DAPQ_PAGES_FP4) {
-    DAPQ_REQUIRE(p->k_scales != nullptr && p->v_scales != nullptr, DAPQ_ERR_INVALID_ARG, "FP4 pages need k_scales and v_scales");
+  if (p->format != DAPQ_PAGES_BF16) {
+    DAPQ_REQUIRE(p->k_scales != nullptr && p->v_scales != nullptr, DAPQ_ERR_INVALID_ARG, "%s pages need k_scales and v_scales",
+                 p->format == DAPQ_PAGES_FP4 ? "FP4" : "E4M3");
     bits |= reinterpret_cast<uintptr_t>(p->k_scales) | reinterpret_cast<uintptr_t>(p->v_scales);
   }
   DAPQ_REQUIRE((bits & 15) == 0, DAPQ_ERR_UNSUPPORTED, "the pools of the pages must be 16-byte aligned");
@@ -80,16 +81,17 @@ __device__ __forceinline__ T get(const T* at) {
 }
 
 // A row of 16 lanes with 8 channels each into the pool.
-template <bool FP4, bool STREAM>
+template <int FMT, bool STREAM>
 __device__ __forceinline__ void put_row16(uint8_t* rows, uint8_t* scales, int64_t row, int ch, u32x4 x) {
-  if constexpr (!FP4) {
+  if constexpr (FMT == kBf16) {
     put<STREAM>(reinterpret_cast<u32x4*>(rows + row * kRowBytes + ch * 16), x);
   } else {
     unsigned m = larger(larger(larger_magnitude(x[0]), larger_magnitude(x[1])), larger(larger_magnitude(x[2]), larger_magnitude(x[3])));
     m = larger(m, dpp<kXor1>(m));
     m = larger(m, dpp<kXor2>(m));
-    const unsigned s = fp4_scale_byte(m);
-    put<STREAM>(reinterpret_cast<unsigned*>(rows + row * kFp4RowBytes + ch * 4), fp4_pack8(x, s));
+    const unsigned s = scale_byte_of<FMT>(m);
+    if constexpr (FMT == kFp4) put<STREAM>(reinterpret_cast<unsigned*>(rows + row * kCodeBytes<kFp4> + ch * 4), fp4_pack8(x, s));
+    else put<STREAM>(reinterpret_cast<u32x2*>(rows + row * kCodeBytes<kE4m3> + ch * 8), e4m3_pack8(x, s));
     unsigned all = s << (8 * (ch >> 2));
     all |= dpp<kRor4>(all);
     all |= dpp<kRor8>(all);
@@ -109,7 +111,7 @@ struct PagedGatherParams {
 
 // As gather_kernel, 16 lanes move a row with one 16-byte load each; a lane group has two rows, and K and V of each, whose place is looked up once.
 // STREAM_IN, STREAM_OUT: hints of the loads and stores of rows.
-template <bool FP4, bool STREAM_IN, bool STREAM_OUT>
+template <int FMT, bool STREAM_IN, bool STREAM_OUT>
 __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherParams p) {
   touch_args<sizeof(PagedGatherParams)>();
   constexpr int ROWS = 2;
@@ -151,8 +153,8 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherParams p) 
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     if (j[r] < 0 || j[r] >= L || to[r] < 0) continue;
-    put_row16<FP4, STREAM_OUT>(p.pool.k, p.pool.k_scales, to[r], ch, x[r][0]);
-    put_row16<FP4, STREAM_OUT>(p.pool.v, p.pool.v_scales, to[r], ch, x[r][1]);
+    put_row16<FMT, STREAM_OUT>(p.pool.k, p.pool.k_scales, to[r], ch, x[r][0]);
+    put_row16<FMT, STREAM_OUT>(p.pool.v, p.pool.v_scales, to[r], ch, x[r][1]);
   }
 }
 
@@ -193,7 +195,7 @@ __device__ __forceinline__ bool find_token(const int32_t* cu_new, int batch, int
 // and 64 + 2c, 65 + 2c, which hold both channels of two pairs in either pairing.  A lane evaluates one angle of the row, in fp64 as
 // dapq_rope_apply does, and has the two that it needs from other lanes.
 // A small call is a chain of trips to memory (one token, 8 heads 4 us); 10000 tokens of 8 heads take 20 us (4.0 TB/s).
-template <bool FP4>
+template <int FMT>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) {
   touch_args<sizeof(PagedAppendParams)>();
   const int lane = threadIdx.x & 63, c = lane & 31;
@@ -242,7 +244,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) 
       }
     }
     const int64_t row = row0 + ((int64_t)hd << p.pool.page_shift);
-    if constexpr (!FP4) {
+    if constexpr (FMT == kBf16) {
       if (mine) {
         unsigned* dst = reinterpret_cast<unsigned*>(rows + row * kRowBytes) + c;
         dst[0] = a;
@@ -254,17 +256,24 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) 
       ma = larger(ma, dpp<kRor2>(ma)), mb = larger(mb, dpp<kRor2>(mb));
       ma = larger(ma, dpp<kRor4>(ma)), mb = larger(mb, dpp<kRor4>(mb));
       ma = larger(ma, dpp<kRor8>(ma)), mb = larger(mb, dpp<kRor8>(mb));
-      const unsigned sa = fp4_scale_byte(ma), sb = fp4_scale_byte(mb);
-      // a byte of each half of the row to a lane; the four of a quad become a dword
-      unsigned ca = sa == kFp4Bad ? 0u : __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2, a), fp4_scale(sa), 0);
-      unsigned cb = sb == kFp4Bad ? 0u : __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2, b), fp4_scale(sb), 0);
-      ca = (ca & 255u) << (8 * (c & 3)), cb = (cb & 255u) << (8 * (c & 3));
-      ca |= dpp<kXor1>(ca), cb |= dpp<kXor1>(cb);
-      ca |= dpp<kXor2>(ca), cb |= dpp<kXor2>(cb);
-      if (mine && (c & 3) == 0) {
-        unsigned* dst = reinterpret_cast<unsigned*>(rows + row * kFp4RowBytes) + (c >> 2);
-        dst[0] = ca;
-        dst[8] = cb;
+      const unsigned sa = scale_byte_of<FMT>(ma), sb = scale_byte_of<FMT>(mb);
+      if constexpr (FMT == kFp4) {
+        // a byte of each half of the row to a lane; the four of a quad become a dword
+        unsigned ca = sa == kNoScale ? 0u : __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2, a), group_scale(sa), 0);
+        unsigned cb = sb == kNoScale ? 0u : __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2, b), group_scale(sb), 0);
+        ca = (ca & 255u) << (8 * (c & 3)), cb = (cb & 255u) << (8 * (c & 3));
+        ca |= dpp<kXor1>(ca), cb |= dpp<kXor1>(cb);
+        ca |= dpp<kXor2>(ca), cb |= dpp<kXor2>(cb);
+        if (mine && (c & 3) == 0) {
+          unsigned* dst = reinterpret_cast<unsigned*>(rows + row * kCodeBytes<kFp4>) + (c >> 2);
+          dst[0] = ca;
+          dst[8] = cb;
+        }
+      } else {
+        // two bytes of each half to a lane; of the two dwords that a pair of lanes has, each stores one
+        unsigned ca = e4m3_pack2(a, sa) << (16 * (c & 1)), cb = e4m3_pack2(b, sb) << (16 * (c & 1));
+        ca |= dpp<kXor1>(ca), cb |= dpp<kXor1>(cb);
+        if (mine) reinterpret_cast<unsigned*>(rows + row * kCodeBytes<kE4m3>)[(c & 1 ? 16 : 0) + (c >> 1)] = c & 1 ? cb : ca;
       }
       if (mine && (c & 15) == 0) {
         scales[row * 4 + (c >> 4)] = (uint8_t)sa;
@@ -285,7 +294,7 @@ struct PagedReadParams {
 };
 
 // 16 lanes to a row, two rows of K and of V to a lane group.
-template <bool FP4, bool STREAM>
+template <int FMT, bool STREAM>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadParams p) {
   touch_args<sizeof(PagedReadParams)>();
   constexpr int ROWS = 2;
@@ -304,26 +313,42 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadParams p) {
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     if (row[r] < 0) continue;
-    if constexpr (FP4) {
-      x[r][0][0] = *reinterpret_cast<const unsigned*>(p.pool.k + row[r] * kFp4RowBytes + ch * 4);
-      x[r][1][0] = *reinterpret_cast<const unsigned*>(p.pool.v + row[r] * kFp4RowBytes + ch * 4);
-      scale[r][0] = p.pool.k_scales[row[r] * 4 + (ch >> 2)];
-      scale[r][1] = p.pool.v_scales[row[r] * 4 + (ch >> 2)];
+    if constexpr (FMT == kFp4) {
+      x[r][0][0] = *reinterpret_cast<const unsigned*>(p.pool.k + row[r] * kCodeBytes<kFp4> + ch * 4);
+      x[r][1][0] = *reinterpret_cast<const unsigned*>(p.pool.v + row[r] * kCodeBytes<kFp4> + ch * 4);
+    } else if constexpr (FMT == kE4m3) {
+      const u32x2 k = get<STREAM>(reinterpret_cast<const u32x2*>(p.pool.k + row[r] * kCodeBytes<kE4m3> + ch * 8));
+      const u32x2 v = get<STREAM>(reinterpret_cast<const u32x2*>(p.pool.v + row[r] * kCodeBytes<kE4m3> + ch * 8));
+      x[r][0][0] = k[0], x[r][0][1] = k[1], x[r][1][0] = v[0], x[r][1][1] = v[1];
     } else {
       x[r][0] = get<STREAM>(reinterpret_cast<const u32x4*>(p.pool.k + row[r] * kRowBytes + ch * 16));
       x[r][1] = get<STREAM>(reinterpret_cast<const u32x4*>(p.pool.v + row[r] * kRowBytes + ch * 16));
+    }
+    if constexpr (FMT != kBf16) {
+      scale[r][0] = p.pool.k_scales[row[r] * 4 + (ch >> 2)];
+      scale[r][1] = p.pool.v_scales[row[r] * 4 + (ch >> 2)];
     }
   }
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     if (row[r] < 0) continue;
-    if constexpr (FP4) {
-      x[r][0] = fp4_unpack8(x[r][0][0], fp4_scale(scale[r][0]));
-      x[r][1] = fp4_unpack8(x[r][1][0], fp4_scale(scale[r][1]));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (FMT == kFp4) x[r][i] = fp4_unpack8(x[r][i][0], group_scale(scale[r][i]));
+      if constexpr (FMT == kE4m3) x[r][i] = e4m3_unpack8(x[r][i][0], x[r][i][1], group_scale(scale[r][i]));
     }
     put<STREAM>(reinterpret_cast<u32x4*>(p.k_out + out + 16 * r * kHeadDim), x[r][0]);
     put<STREAM>(reinterpret_cast<u32x4*>(p.v_out + out + 16 * r * kHeadDim), x[r][1]);
   }
+}
+
+template <int FMT>
+auto gather_of(int64_t moved) {
+  return moved >= kStreamIn ? paged_gather_kernel<FMT, true, true> : (moved >= kStreamOut ? paged_gather_kernel<FMT, false, true> : paged_gather_kernel<FMT, false, false>);
+}
+template <int FMT>
+auto read_of(int64_t moved) {
+  return moved >= kStreamRead ? paged_read_kernel<FMT, true> : paged_read_kernel<FMT, false>;
 }
 
 }  // namespace
@@ -361,13 +386,9 @@ extern "C" DAPQ_API int dapq_paged_gather(const dapq_shape* shape, const dapq_pa
   const int64_t rows = (int64_t)pages->max_pages * pages->page_rows;
   const unsigned blocks = (unsigned)(((budget < rows ? budget : rows) + 31) / 32);
   // bytes read and written where every head keeps its whole budget
-  const int64_t moved = (int64_t)shape->n_layers * shape->batch * shape->n_kv_heads * (budget < rows ? budget : rows) * 2 *
-                        (kRowBytes + (pages->format == DAPQ_PAGES_FP4 ? kFp4RowBytes + 4 : kRowBytes));
+  const int64_t moved = (int64_t)shape->n_layers * shape->batch * shape->n_kv_heads * (budget < rows ? budget : rows) * 2 * (kRowBytes + row_bytes(pages));
   DAPQ_REQUIRE((uint64_t)blocks * 256 < (uint64_t)1 << 32, DAPQ_ERR_UNSUPPORTED, "budget (%d) is too large", budget);
-  const bool fp4 = pages->format == DAPQ_PAGES_FP4;
-  auto kernel = fp4 ? paged_gather_kernel<true, false, false> : paged_gather_kernel<false, false, false>;
-  if (moved >= kStreamOut) kernel = fp4 ? paged_gather_kernel<true, false, true> : paged_gather_kernel<false, false, true>;
-  if (moved >= kStreamIn) kernel = fp4 ? paged_gather_kernel<true, true, true> : paged_gather_kernel<false, true, true>;
+  auto kernel = pages->format == DAPQ_PAGES_BF16 ? gather_of<kBf16>(moved) : (pages->format == DAPQ_PAGES_FP4 ? gather_of<kFp4>(moved) : gather_of<kE4m3>(moved));
   hipLaunchKernelGGL(kernel, dim3(blocks, (unsigned)(shape->n_layers * shape->n_kv_heads), (unsigned)shape->batch), dim3(256), 0,
                      static_cast<hipStream_t>(stream), p);
   DAPQ_HIP_LAUNCH_CHECK("paged_gather_kernel");
@@ -410,7 +431,7 @@ extern "C" DAPQ_API int dapq_paged_append(const dapq_pages* pages, const dapq_st
   p.run = 2;
   while (p.run < 32 && p.run < pages->n_kv_heads && step->total_new * pages->n_layers * ((pages->n_kv_heads + 2 * p.run - 1) / (2 * p.run)) >= 2048) p.run *= 2;
   p.k_runs = (pages->n_kv_heads + p.run - 1) / p.run;
-  hipLaunchKernelGGL(pages->format == DAPQ_PAGES_FP4 ? paged_append_kernel<true> : paged_append_kernel<false>,
+  hipLaunchKernelGGL(pages->format == DAPQ_PAGES_BF16 ? paged_append_kernel<kBf16> : (pages->format == DAPQ_PAGES_FP4 ? paged_append_kernel<kFp4> : paged_append_kernel<kE4m3>),
                      dim3((unsigned)((step->total_new + 3) / 4), (unsigned)(2 * p.k_runs), (unsigned)pages->n_layers), dim3(256), 0,
                      static_cast<hipStream_t>(stream), p);
   DAPQ_HIP_LAUNCH_CHECK("paged_append_kernel");
@@ -434,10 +455,8 @@ extern "C" DAPQ_API int dapq_paged_read(const dapq_pages* pages, const int32_t* 
   const int64_t rows = (int64_t)pages->max_pages * pages->page_rows;  // (below 2^30: 2^33 threads would be too many)
   const uint64_t blocks = (uint64_t)(((max_rows < rows ? max_rows : rows) + 31) / 32);
   DAPQ_REQUIRE(blocks * 256 < (uint64_t)1 << 32, DAPQ_ERR_UNSUPPORTED, "max_rows (%d) is too large", max_rows);
-  const int64_t moved = (int64_t)pages->n_layers * pages->batch * pages->n_kv_heads * (max_rows < rows ? max_rows : rows) * 2 *
-                        (kRowBytes + (pages->format == DAPQ_PAGES_FP4 ? kFp4RowBytes + 4 : kRowBytes));
-  auto kernel = pages->format == DAPQ_PAGES_FP4 ? (moved >= kStreamRead ? paged_read_kernel<true, true> : paged_read_kernel<true, false>)
-                                                : (moved >= kStreamRead ? paged_read_kernel<false, true> : paged_read_kernel<false, false>);
+  const int64_t moved = (int64_t)pages->n_layers * pages->batch * pages->n_kv_heads * (max_rows < rows ? max_rows : rows) * 2 * (kRowBytes + row_bytes(pages));
+  auto kernel = pages->format == DAPQ_PAGES_BF16 ? read_of<kBf16>(moved) : (pages->format == DAPQ_PAGES_FP4 ? read_of<kFp4>(moved) : read_of<kE4m3>(moved));
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)(pages->n_layers * pages->n_kv_heads), (unsigned)pages->batch), dim3(256), 0,
                      static_cast<hipStream_t>(stream), p);
   DAPQ_HIP_LAUNCH_CHECK("paged_read_kernel");

@@ -85,7 +85,7 @@ struct Part {
 // instructions a tile begin to count: three waves to a SIMD, two take 63); one item alone takes 0.27 us a tile in bf16, 0.16 in 4 bits, behind 5 to 6 us.
 // BLOCKS: blocks of 16 columns; 0: up to 8 columns, whose leading and following parts take the two halves of one block.
 // SPLIT: a workgroup has a part of an item; else an item (and nothing is to be joined).
-template <bool FP4, int BLOCKS, int CAP, bool SPLIT>
+template <int FMT, int BLOCKS, int CAP, bool SPLIT>
 __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_rows_kernel(PagedAttentionParams p) {
   touch_args<sizeof(PagedAttentionParams)>();
   constexpr bool kHalf = BLOCKS == 0;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (kQueriesInLds && 2 * t + (i >> 1) != wave) continue;
-        const bf16x8 x = *reinterpret_cast<const bf16x8*>(src + (FP4 ? 32 * kg + 8 * i : 32 * i + 8 * kg));
+        const bf16x8 x = *reinterpret_cast<const bf16x8*>(src + (FMT == kBf16 ? 32 * i + 8 * kg : 32 * kg + 8 * i));
         if constexpr (kQueriesInLds) queries[(t * 4 + i) * 64 + lane] = x;
         else qf[t][i] = x;
       }
@@ -197,40 +197,45 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
     };
     // A tile in registers.  Keys: the operand (bf16), or a row's group of 32 channels to a lane.  Values: 8 channels of the rows
     // 16 * (e / 4) + 4 * kg + e % 4.
+    constexpr int kBytes = kCodeBytes<FMT>, kKeyLoads = FMT == kBf16 ? 4 : kBytes / 64;
     struct Buffer {
-      u32x4 kf[2][FP4 ? 1 : 4];
+      u32x4 kf[2][kKeyLoads];
       unsigned ks[2];
-      u32x4 vt[FP4 ? 1 : 8];
-      unsigned vc[8];
+      u32x4 vt[FMT == kBf16 ? 8 : 1];
+      unsigned vc[8][FMT == kE4m3 ? 2 : 1];
       u32x4 vs[2];
       Rows rows;
     };
     Buffer b;
     // (through descriptors of 16 rows each: the address of a lane is an offset of 32 bits, and what is on no page is not read)
-    const unsigned k_at = n * (FP4 ? kFp4RowBytes : kRowBytes) + kg * 16, v_at = 4 * kg * (FP4 ? kFp4RowBytes : kRowBytes) + n * (FP4 ? 4 : 16);
+    const unsigned k_at = n * kBytes + kg * (FMT == kBf16 ? 16 : kBytes / 4), v_at = 4 * kg * kBytes + n * (kBytes / 16);
     auto rows16 = [&](uint8_t* pool, const Rows& r, int hf, int bytes) {
       return __builtin_amdgcn_make_buffer_rsrc(pool + (uint64_t)(r.ok[hf] ? r.at[hf] : 0) * (16 * bytes), 0, r.ok[hf] ? 16 * bytes : 0, 0x00020000);
     };
     auto load_k = [&](const Rows& r) {
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        const auto src = rows16(p.pool.k, r, hf, FP4 ? kFp4RowBytes : kRowBytes);
+        const auto src = rows16(p.pool.k, r, hf, kBytes);
 #pragma unroll
-        for (int i = 0; i < (FP4 ? 1 : 4); ++i) b.kf[hf][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)k_at + i * 64, 0, 0));
-        if constexpr (FP4) b.ks[hf] = __builtin_amdgcn_raw_buffer_load_b8(rows16(p.pool.k_scales, r, hf, 4), n * 4 + kg, 0, 0);
+        for (int i = 0; i < kKeyLoads; ++i) b.kf[hf][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)k_at + i * (FMT == kBf16 ? 64 : 16), 0, 0));
+        if constexpr (FMT != kBf16) b.ks[hf] = __builtin_amdgcn_raw_buffer_load_b8(rows16(p.pool.k_scales, r, hf, 4), n * 4 + kg, 0, 0);
       }
     };
     auto load_v = [&](const Rows& r) {
       b.rows = r;
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        const auto src = rows16(p.pool.v, r, hf, FP4 ? kFp4RowBytes : kRowBytes);
+        const auto src = rows16(p.pool.v, r, hf, kBytes);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if constexpr (FP4) b.vc[4 * hf + e] = __builtin_amdgcn_raw_buffer_load_b32(src, (int)v_at + e * kFp4RowBytes, 0, 0);
-          else b.vt[4 * hf + e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)v_at + e * kRowBytes, 0, 0));
+          if constexpr (FMT == kFp4) {
+            b.vc[4 * hf + e][0] = __builtin_amdgcn_raw_buffer_load_b32(src, (int)v_at + e * kBytes, 0, 0);
+          } else if constexpr (FMT == kE4m3) {
+            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(src, (int)v_at + e * kBytes, 0, 0));
+            b.vc[4 * hf + e][0] = x[0], b.vc[4 * hf + e][1] = x[1];
+          } else b.vt[4 * hf + e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (int)v_at + e * kRowBytes, 0, 0));
         }
-        if constexpr (FP4) b.vs[hf] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows16(p.pool.v_scales, r, hf, 4), 16 * kg, 0, 0));
+        if constexpr (FMT != kBf16) b.vs[hf] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows16(p.pool.v_scales, r, hf, 4), 16 * kg, 0, 0));
       }
     };
 
@@ -261,7 +266,8 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           u32x4 a;
-          if constexpr (FP4) a = fp4_unpack8(b.kf[hf][0][i], fp4_scale(b.ks[hf]));
+          if constexpr (FMT == kFp4) a = fp4_unpack8(b.kf[hf][0][i], group_scale(b.ks[hf]));
+          else if constexpr (FMT == kE4m3) a = e4m3_unpack8(b.kf[hf][i >> 1][2 * (i & 1)], b.kf[hf][i >> 1][2 * (i & 1) + 1], group_scale(b.ks[hf]));
           else a = b.kf[hf][i];
 #pragma unroll
           for (int t = 0; t < NB; ++t)
@@ -323,9 +329,9 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
           lo[t][e] = __builtin_amdgcn_perm(w2[2 * e + 1], w2[2 * e], 0x07060302u);
         }
       }
-      float vscale[8];  // FP4: of the rows, for this lane's channels
+      float vscale[8];  // codes: of the rows, for this lane's channels
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vscale[e] = FP4 ? fp4_scale((b.vs[e >> 2][e & 3] >> (8 * (n >> 2))) & 255u) : 0.0f;
+      for (int e = 0; e < 8; ++e) vscale[e] = FMT != kBf16 ? group_scale((b.vs[e >> 2][e & 3] >> (8 * (n >> 2))) & 255u) : 0.0f;
       if (partial) {
         // Rows that no column sees may hold anything, and 0 times it must be 0.  A value that is infinite or no number, in a row that some columns
         // see and others don't, is added to the former by itself, in LDS.
@@ -335,12 +341,18 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
         for (int e = 0; e < 8; ++e) {
           const int row = row0 + 16 * (e >> 2) + 4 * kg + (e & 3);
           const bool none = row >= seen_by_last || !now.ok[e >> 2];
-          if constexpr (FP4) {
+          if constexpr (FMT == kFp4) {
             if (none) {
-              b.vc[e] = 0;
+              b.vc[e][0] = 0;
               vscale[e] = 1.0f;
             }
             top = fmaxf(top, row >= seen_by_all ? vscale[e] : 0.0f);
+          } else if constexpr (FMT == kE4m3) {
+            if (none) {
+              b.vc[e][0] = b.vc[e][1] = 0;
+              vscale[e] = 1.0f;
+            }
+            odd |= row >= seen_by_all && (e4m3_past(b.vc[e][0], vscale[e]) | e4m3_past(b.vc[e][1], vscale[e])) != 0;
           } else {
             if (none) b.vt[e] = u32x4{0, 0, 0, 0};
             if (row >= seen_by_all) {
@@ -353,12 +365,13 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
             }
           }
         }
-        if (__any(odd || top > kLargestFp4Scale)) {
-          if constexpr (FP4) {
+        if (__any(odd || top > kLargestScale<kFp4>)) {
+          if constexpr (FMT != kBf16) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               if (row0 + 16 * (e >> 2) + 4 * kg + (e & 3) < seen_by_all) continue;
-              b.vc[e] = fp4_finite8(b.vc[e], vscale[e]);
+              if constexpr (FMT == kFp4) b.vc[e][0] = fp4_finite8(b.vc[e][0], vscale[e]);
+              else b.vc[e][0] = e4m3_finite4(b.vc[e][0], vscale[e]), b.vc[e][1] = e4m3_finite4(b.vc[e][1], vscale[e]);
               if (vscale[e] > 0x1p127f) vscale[e] = 1.0f;  // (0 without a scale is no number)
             }
           }
@@ -372,7 +385,9 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
             if (!(i < 16 ? now.ok[0] : now.ok[1])) continue;
             const int64_t at = (int64_t)(i < 16 ? now.at[0] : now.at[1]) * 16 + (i & 15);
             unsigned u;
-            if constexpr (FP4) u = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((unsigned)p.pool.v[at * kFp4RowBytes + lane], fp4_scale(p.pool.v_scales[at * 4 + (lane >> 4)]), 0));
+            if constexpr (FMT == kFp4) u = fp4_unpack2((unsigned)p.pool.v[at * kBytes + lane], group_scale(p.pool.v_scales[at * 4 + (lane >> 4)]), 0);
+            else if constexpr (FMT == kE4m3)
+              u = e4m3_unpack2(*reinterpret_cast<const uint16_t*>(p.pool.v + at * kBytes + 2 * lane), group_scale(p.pool.v_scales[at * 4 + (lane >> 4)]), 0);
             else u = *reinterpret_cast<const unsigned*>(p.pool.v + at * kRowBytes + lane * 4);
             u &= infinite_bits(u);
             if (!__any(u != 0)) continue;
@@ -390,7 +405,8 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
         unsigned x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          if constexpr (FP4) x[e] = fp4_unpack2(b.vc[e], vscale[e], i);
+          if constexpr (FMT == kFp4) x[e] = fp4_unpack2(b.vc[e][0], vscale[e], i);
+          else if constexpr (FMT == kE4m3) x[e] = e4m3_unpack2(b.vc[e][i >> 1], vscale[e], i & 1);
           else x[e] = b.vt[e][i];
         }
 #pragma unroll
@@ -599,12 +615,12 @@ RowPlan row_plan(const dapq_pages* p, int cols) {
   return plan;
 }
 
-template <bool FP4, int BLOCKS, bool SPLIT>
+template <int FMT, int BLOCKS, bool SPLIT>
 int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, hipStream_t stream) {
   constexpr int kCols = BLOCKS == 0 ? 8 : 16 * BLOCKS, kBytes = kRowWaves * (BLOCKS == 0 ? 1 : BLOCKS) * 16 * (kHeadDim + 2) * 4 + (BLOCKS == 2 ? 8192 : 0);
   const Cap cap = cap_of(p);
-  auto kernel = cap == kNoCap ? paged_rows_kernel<FP4, BLOCKS, kNoCap, SPLIT>
-                              : (cap == kSmallCap ? paged_rows_kernel<FP4, BLOCKS, kSmallCap, SPLIT> : paged_rows_kernel<FP4, BLOCKS, kLargeCap, SPLIT>);
+  auto kernel = cap == kNoCap ? paged_rows_kernel<FMT, BLOCKS, kNoCap, SPLIT>
+                              : (cap == kSmallCap ? paged_rows_kernel<FMT, BLOCKS, kSmallCap, SPLIT> : paged_rows_kernel<FMT, BLOCKS, kLargeCap, SPLIT>);
   const int rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), kBytes);
   if (rc != DAPQ_OK) return rc;
   const unsigned items = (unsigned)(pages->batch * p.items);  // (below 2^24)
@@ -618,17 +634,18 @@ int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, hipStrea
   }
   return DAPQ_OK;
 }
-template <bool FP4, bool SPLIT>
+template <int FMT, bool SPLIT>
 int launch_rows(const dapq_pages* pages, const PagedAttentionParams& p, int cols, hipStream_t stream) {
-  return cols == 8 ? launch_rows<FP4, 0, SPLIT>(pages, p, stream) : (cols == 16 ? launch_rows<FP4, 1, SPLIT>(pages, p, stream) : launch_rows<FP4, 2, SPLIT>(pages, p, stream));
+  return cols == 8 ? launch_rows<FMT, 0, SPLIT>(pages, p, stream) : (cols == 16 ? launch_rows<FMT, 1, SPLIT>(pages, p, stream) : launch_rows<FMT, 2, SPLIT>(pages, p, stream));
 }
 int launch_rows(const dapq_pages* pages, PagedAttentionParams p, int cols, hipStream_t stream) {
   const RowPlan plan = row_plan(pages, cols);
   p.groups = plan.groups;
   p.spare = plan.spare;
   p.inv_spare = 1.0f / (float)plan.spare;
-  if (pages->format == DAPQ_PAGES_FP4) return plan.split ? launch_rows<true, true>(pages, p, cols, stream) : launch_rows<true, false>(pages, p, cols, stream);
-  return plan.split ? launch_rows<false, true>(pages, p, cols, stream) : launch_rows<false, false>(pages, p, cols, stream);
+  if (pages->format == DAPQ_PAGES_FP4) return plan.split ? launch_rows<kFp4, true>(pages, p, cols, stream) : launch_rows<kFp4, false>(pages, p, cols, stream);
+  if (pages->format == DAPQ_PAGES_E4M3) return plan.split ? launch_rows<kE4m3, true>(pages, p, cols, stream) : launch_rows<kE4m3, false>(pages, p, cols, stream);
+  return plan.split ? launch_rows<kBf16, true>(pages, p, cols, stream) : launch_rows<kBf16, false>(pages, p, cols, stream);
 }
 
 int check_attention(const dapq_pages* pages, const dapq_step* step) {

@@ -8,7 +8,6 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTurnTile = 64;   // cache rows of a tile
 constexpr int kTurnWaves = 4;
@@ -61,7 +60,7 @@ __device__ __forceinline__ int find_block(const TurnParams& p, int lane, int* bl
 // the other half's products: 396..404.
 // Weights enter as one bf16, rounded to nearest: an error of 2^-9 of a weight, independent from row to row, below the rounding of the result where
 // more than a few rows count; a second part would take half as many matrix instructions again.
-template <bool FP4, int CAP, bool SPLIT>
+template <int FMT, int CAP, bool SPLIT>
 __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_kernel(TurnParams p) {
   extern __shared__ char lds[];  // K of two tiles, V of two tiles; flags of four tiles
   // of a tile: 1 for values that are not finite, 2 << i for rows 16 * i .. on no page.  Tile t's are written in step t - 1, read in step t and cleared
@@ -106,7 +105,8 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
 
   // Bringing in: this wave's rows of a tile, in registers, then in LDS.
   const int32_t* table = p.pool.table + (int64_t)seq * p.pool.max_pages;
-  u32x4 kr[FP4 ? 1 : kTurnRows / 4], vr[FP4 ? 1 : kTurnRows / 4];
+  constexpr int kBytes = kCodeBytes<FMT>, kLoads = kTurnRows * kBytes / 1024;
+  u32x4 kr[kLoads], vr[kLoads];  // bf16: load j has row 4 * j + lane / 16; codes: a lane has a group of row lane / 4
   unsigned ks = 0, vs = 0;
   int loaded_row = 0;  // the first of the rows in the registers
   bool loaded_page = false;
@@ -124,15 +124,15 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
     int rows = seen_by_last - loaded_row;
     rows = uniform(page < 0 || rows < 0 ? 0 : (rows < kTurnRows ? rows : kTurnRows));
     const int64_t at = uniform64(page_row(p.pool, layer, page < 0 ? 0 : page, head) + (loaded_row & ((1 << p.pool.page_shift) - 1)));
-    constexpr int kBytes = FP4 ? kFp4RowBytes : kRowBytes;
     const auto ksrc = __builtin_amdgcn_make_buffer_rsrc(p.pool.k + at * kBytes, 0, rows * kBytes, 0x00020000);  // (past the rows: zeros)
     const auto vsrc = __builtin_amdgcn_make_buffer_rsrc(p.pool.v + at * kBytes, 0, rows * kBytes, 0x00020000);
 #pragma unroll
-    for (int j = 0; j < (FP4 ? 1 : kTurnRows / 4); ++j) {
-      kr[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ksrc, lane * 16 + j * 1024, 0, 0));
-      vr[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vsrc, lane * 16 + j * 1024, 0, 0));
+    for (int j = 0; j < kLoads; ++j) {
+      const int at_lane = FMT == kBf16 ? lane * 16 + j * 1024 : lane * (kBytes / 4) + j * 16;
+      kr[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ksrc, at_lane, 0, 0));
+      vr[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vsrc, at_lane, 0, 0));
     }
-    if constexpr (FP4) {
+    if constexpr (FMT != kBf16) {
       ks = __builtin_amdgcn_raw_buffer_load_b8(__builtin_amdgcn_make_buffer_rsrc(p.pool.k_scales + at * 4, 0, rows * 4, 0x00020000), lane, 0, 0);
       vs = __builtin_amdgcn_raw_buffer_load_b8(__builtin_amdgcn_make_buffer_rsrc(p.pool.v_scales + at * 4, 0, rows * 4, 0x00020000), lane, 0, 0);
     }
@@ -141,19 +141,29 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
     char* kt = lds + buffer * kTurnTileBytes;
     char* vt = kt + 2 * kTurnTileBytes;
     bool odd = false;  // a value that is not finite in a row that some columns see and others don't: 0 times it would not be 0
-    if constexpr (FP4) {
+    if constexpr (FMT != kBf16) {
       const int row = kTurnRows * wave + (lane >> 2);
-      float scale = fp4_scale(vs);
-      if (loaded_row + (lane >> 2) >= seen_by_all && scale > kLargestFp4Scale) {
+      float scale = group_scale(vs);
+      bool past = false;
+      if (loaded_row + (lane >> 2) >= seen_by_all) {
+        if constexpr (FMT == kFp4) past = scale > kLargestScale<kFp4>;
+        else
+#pragma unroll
+          for (int i = 0; i < 4 * kLoads; ++i) past |= e4m3_past(vr[i >> 2][i & 3], scale) != 0;
+      }
+      if (past) {
         odd = true;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) vr[0][i] = fp4_finite8(vr[0][i], scale);
+        for (int i = 0; i < 4 * kLoads; ++i) vr[i >> 2][i & 3] = FMT == kFp4 ? fp4_finite8(vr[i >> 2][i & 3], scale) : e4m3_finite4(vr[i >> 2][i & 3], scale);
         if (scale > 0x1p127f) scale = 1.0f;  // (0 without a scale is no number)
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        *reinterpret_cast<u32x4*>(kt + chunk_at(row, 4 * (lane & 3) + i)) = fp4_unpack8(kr[0][i], fp4_scale(ks));
-        *reinterpret_cast<u32x4*>(vt + chunk_at(row, 4 * (lane & 3) + i)) = fp4_unpack8(vr[0][i], scale);
+        u32x4 k, v;
+        if constexpr (FMT == kFp4) k = fp4_unpack8(kr[0][i], group_scale(ks)), v = fp4_unpack8(vr[0][i], scale);
+        else k = e4m3_unpack8(kr[i >> 1][2 * (i & 1)], kr[i >> 1][2 * (i & 1) + 1], group_scale(ks)), v = e4m3_unpack8(vr[i >> 1][2 * (i & 1)], vr[i >> 1][2 * (i & 1) + 1], scale);
+        *reinterpret_cast<u32x4*>(kt + chunk_at(row, 4 * (lane & 3) + i)) = k;
+        *reinterpret_cast<u32x4*>(vt + chunk_at(row, 4 * (lane & 3) + i)) = v;
       }
     } else {
 #pragma unroll
@@ -276,11 +286,16 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
           for (int i4 = 0; i4 < 4; ++i4) {
             const int c = 32 * cb + 8 * i4 + four;
             unsigned x[2];
-            if constexpr (FP4) {
-              const unsigned codes = *reinterpret_cast<const uint16_t*>(p.pool.v + at * kFp4RowBytes + c / 2);
-              const float scale = fp4_scale(p.pool.v_scales[at * 4 + cb]);
+            if constexpr (FMT == kFp4) {
+              const unsigned codes = *reinterpret_cast<const uint16_t*>(p.pool.v + at * kBytes + c / 2);
+              const float scale = group_scale(p.pool.v_scales[at * 4 + cb]);
               x[0] = fp4_unpack2(codes, scale, 0);
               x[1] = fp4_unpack2(codes, scale, 1);
+            } else if constexpr (FMT == kE4m3) {
+              const unsigned codes = *reinterpret_cast<const unsigned*>(p.pool.v + at * kBytes + c);
+              const float scale = group_scale(p.pool.v_scales[at * 4 + cb]);
+              x[0] = e4m3_unpack2(codes, scale, 0);
+              x[1] = e4m3_unpack2(codes, scale, 1);
             } else {
               const u32x2 u = *reinterpret_cast<const u32x2*>(p.pool.v + at * kRowBytes + c * 2);
               x[0] = u[0];
@@ -412,12 +427,12 @@ TurnPlan turn_plan(const dapq_pages* pages, const dapq_step* step) {
   return plan;
 }
 
-template <bool FP4, bool SPLIT>
+template <int FMT, bool SPLIT>
 int launch_turn(const TurnParams& p, hipStream_t stream) {
   constexpr int kBytes = 4 * kTurnTileBytes + 16;
   const Cap cap = cap_of(p);
-  auto kernel = cap == kNoCap ? paged_turn_kernel<FP4, kNoCap, SPLIT>
-                              : (cap == kSmallCap ? paged_turn_kernel<FP4, kSmallCap, SPLIT> : paged_turn_kernel<FP4, kLargeCap, SPLIT>);
+  auto kernel = cap == kNoCap ? paged_turn_kernel<FMT, kNoCap, SPLIT>
+                              : (cap == kSmallCap ? paged_turn_kernel<FMT, kSmallCap, SPLIT> : paged_turn_kernel<FMT, kLargeCap, SPLIT>);
   const int rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), kBytes);
   if (rc != DAPQ_OK) return rc;
   hipLaunchKernelGGL(kernel, dim3((unsigned)p.blocks * p.items, (unsigned)p.splits), dim3(64 * kTurnWaves), kBytes, stream, p);
@@ -444,8 +459,9 @@ int launch_turn(const dapq_pages* pages, const dapq_step* step, const PagedAtten
                (long long)(plan.blocks * p.items), kTurnCols);
   p.blocks = (int32_t)plan.blocks;
   p.splits = plan.splits;
-  if (pages->format == DAPQ_PAGES_FP4) return p.splits > 1 ? launch_turn<true, true>(p, stream) : launch_turn<true, false>(p, stream);
-  return p.splits > 1 ? launch_turn<false, true>(p, stream) : launch_turn<false, false>(p, stream);
+  if (pages->format == DAPQ_PAGES_FP4) return p.splits > 1 ? launch_turn<kFp4, true>(p, stream) : launch_turn<kFp4, false>(p, stream);
+  if (pages->format == DAPQ_PAGES_E4M3) return p.splits > 1 ? launch_turn<kE4m3, true>(p, stream) : launch_turn<kE4m3, false>(p, stream);
+  return p.splits > 1 ? launch_turn<kBf16, true>(p, stream) : launch_turn<kBf16, false>(p, stream);
 }
 
 }  // namespace dapq

@@ -34,6 +34,9 @@ class Cache:
         if fmt == "fp4":
             self.pool = {"k": np.full(shape + (64,), 0x77, np.uint8), "v": np.full(shape + (64,), 0x77, np.uint8),
                          "k_scales": np.full(shape + (4,), 255, np.uint8), "v_scales": np.full(shape + (4,), 255, np.uint8)}
+        elif fmt == "e4m3":
+            self.pool = {"k": np.full(shape + (128,), 0x7f, np.uint8), "v": np.full(shape + (128,), 0x7f, np.uint8),
+                         "k_scales": np.full(shape + (4,), 255, np.uint8), "v_scales": np.full(shape + (4,), 255, np.uint8)}
         else:
             self.pool = {"k": np.full(shape + (128,), JUNK, np.uint16), "v": np.full(shape + (128,), JUNK, np.uint16)}
 
@@ -47,8 +50,9 @@ class Cache:
                 page, slot = where
                 for name, g in (("k", gain), ("v", 1.0)):
                     x = rng.standard_normal((self.layers, self.heads, 128)) * g
-                    if self.fmt == "fp4":
-                        self.pool[name][:, page, :, slot], self.pool[name + "_scales"][:, page, :, slot] = PO.fp4_quantise(x)
+                    if self.fmt != "bf16":
+                        quantise = PO.fp4_quantise if self.fmt == "fp4" else PO.e4m3_quantise
+                        self.pool[name][:, page, :, slot], self.pool[name + "_scales"][:, page, :, slot] = quantise(x)
                     else:
                         self.pool[name][:, page, :, slot] = O.f64_to_bf16_bits(x)
         return self
