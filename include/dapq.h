@@ -384,6 +384,69 @@ int dapq_paged_attention(const dapq_pages* pages, const dapq_step* step, const v
 /* Bytes of device workspace dapq_paged_attention needs (0 if the arguments are invalid: the call itself then reports why). */
 size_t dapq_paged_attention_workspace_bytes(const dapq_pages* pages, const dapq_step* step);
 
+/* --- Steps that read chosen blocks of a cache in pages -----------------------------------------------------------------
+ * What an eviction kept, and what turns have added, is read whole by dapq_paged_attention for every token.  The calls below let every token read those
+ * blocks of rows only that its queries can score highest.  dapq_paged_bounds notes the bounds of a block's keys, channel by channel, once its rows are there;
+ * dapq_paged_select takes a bound of every block's scores from them and keeps the highest; dapq_paged_sparse_attention attends to the rows of the kept blocks.
+ *
+ * Block b of a sequence and KV head is the rows b * block_rows .. b * block_rows + block_rows - 1: a part of one page, block number
+ * B = R / block_rows with R the row number of its first row in the pool (dapq_pages).  Bounds and scales belong to the pool as its rows do: sequences that
+ * share a page share its blocks' bounds. */
+typedef struct dapq_blocks {
+  int32_t block_rows;     /* 16, 32, 64, ... up to the pages' page_rows */
+  int32_t n_select;       /* blocks that a token's queries of a KV head read, at most; 1 to 4096 */
+  int32_t n_first;        /* among them the first blocks of the sequence, however they score (>= 0) */
+  int32_t n_last;         /* and the last ones that the token sees (>= 1); n_first + n_last <= n_select */
+  int8_t* bounds;         /* device, 16-byte aligned: int8 [2][128] at byte 256 * B, the upper bounds of the channels, then the lower ones */
+  uint8_t* scales;        /* device: one byte at B; scale byte s multiplies the block's bounds by 2^(s - 127), 255 stands for a key that is not finite */
+} dapq_blocks;
+
+/* The bounds of the blocks that rows first[seq] .. lengths[seq] - 1 complete: of every block b of a sequence with
+ *   first[seq] < (b + 1) * block_rows <= lengths[seq]
+ * on a page, upper[c] = ceil(max_j k_j[c] / 2^e) and lower[c] = floor(min_j k_j[c] / 2^e) over its rows, as what attention reads (FP4 and E4M3: the
+ * values of the codes), with the least e in [-50, 50] at which every |k_j[c]| <= 127 * 2^e; bounds past 127 (keys past 127 * 2^50) are 127.
+ * Scale byte e + 127; a block with a key that is infinite or no number gets 255 and bounds of 0.  Other blocks are left as they were.
+ *   first     device, int32 [batch], or NULL: 0 (every complete block, after dapq_paged_gather say); negative counts as 0
+ *   lengths   device, int32 [batch]: rows that each sequence holds now
+ *   max_rows  no lengths[seq] - first[seq] is more than this (of a sequence where it is, the first blocks are written: those up to row first[seq] + max_rows)
+ * Uses block_rows, bounds and scales of blocks.  While decoding: behind dapq_paged_append with first = the step's lengths, and the lengths behind it. */
+int dapq_paged_bounds(const dapq_pages* pages, const dapq_blocks* blocks, const int32_t* first, const int32_t* lengths, int32_t max_rows, void* stream);
+
+/* The blocks that each new token's queries read, for every KV head.  Token t of sequence seq sees n = lengths[seq] + t + 1 rows, and the blocks
+ * 0 .. ceil(n / block_rows) - 1 as far as they are on a page; it reads all of them if they are no more than n_select, else the first n_first, the last
+ * n_last of ceil(n / block_rows), and of the others those with the highest score, of equal scores those that come first, n_select in all.
+ * The score of a block is a bound of scores q.k:  the query is rounded to whole numbers u[c] (nearest, ties to even), |u| <= 127, of 2^f with the
+ * least f in [-50, 50] at which every |q[c]| <= 127 * 2^f (past 127 * 2^50: 127; a query with an infinity or a NaN counts as 0),
+ *   score = max over the query heads of the KV head of  2^(f + e) * sum_c max(u[c] * upper[c], u[c] * lower[c]),
+ * which is exact in fp32, so that the choice is the same however it is computed.  A block whose scale byte is 255 comes before all that are scored.
+ * Bounds of the first n_first blocks and of the last n_last ones that a token sees are not read, so that it is enough that complete blocks have them; the
+ * scale bytes of the others have to be 77 .. 177, or 255, as dapq_paged_bounds writes them.
+ *   q      device, bf16, rotated, as for dapq_paged_attention (the q strides of step)
+ *   idx    out, int32 [n_layers][total_new][n_kv_heads][n_select]: blocks, ascending; entries past count are left as they were
+ *   count  out, int32 [n_layers][total_new][n_kv_heads]; idx and count of tokens past max_new are left as they were
+ *   workspace  device scratch of at least dapq_paged_select_workspace_bytes(pages, blocks, step), 256-byte aligned: scores of the blocks.  The figure depends
+ *        on neither the lengths nor cu_new.
+ * Uses the table of pages, all of blocks, and n_q_heads, max_new, total_new, cu_new, lengths and the q strides of step. */
+int dapq_paged_select(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, const void* q, int32_t* idx, int32_t* count,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace dapq_paged_select needs (0 if the arguments are invalid: the call itself then reports why). */
+size_t dapq_paged_select_workspace_bytes(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step);
+
+/* dapq_paged_attention over the rows of chosen blocks: token t of sequence seq and query head h attend to the rows j <= lengths[seq] + t on a page
+ * of the blocks idx[layer][cu_new[seq] + t][kv_head][0 .. count - 1], in the format of dapq_paged_select.  An entry that is no block of the table has no rows;
+ * blocks may stand in any order, and one that is named twice counts twice.  A count past n_select counts as n_select, a negative one as 0.
+ *   q, out     as for dapq_paged_attention; 0 where no row is visible
+ *   workspace  device scratch of at least dapq_paged_sparse_attention_workspace_bytes(pages, blocks, step), 256-byte aligned
+ * Uses block_rows and n_select of blocks (bounds and scales may be NULL), and what dapq_paged_attention uses of step, softcap too.  Sums, weights
+ * and values that are not finite are as in dapq_paged_attention of few query rows.  The work is that of the chosen rows, read anew for every token: a
+ * turn of many tokens behind a cache that is not many times longer than n_select * block_rows is done sooner by dapq_paged_attention. */
+int dapq_paged_sparse_attention(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, const void* q, const int32_t* idx,
+                                const int32_t* count, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace dapq_paged_sparse_attention needs (0 if the arguments are invalid: the call itself then reports why). */
+size_t dapq_paged_sparse_attention_workspace_bytes(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step);
+
 #ifdef __cplusplus
 }
 #endif

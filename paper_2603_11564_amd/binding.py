@@ -23,6 +23,7 @@ EXPORTS = (
     "dapq_score_accumulate", "dapq_score_stats_extend", "dapq_pool", "dapq_topk", "dapq_pool_topk", "dapq_topk_workspace_bytes", "dapq_gather", "dapq_recall", "dapq_decode_attention",
     "dapq_score_static", "dapq_score_static_capacity", "dapq_score_single_launch",
     "dapq_paged_gather", "dapq_paged_append", "dapq_paged_read", "dapq_paged_attention", "dapq_paged_attention_workspace_bytes",
+    "dapq_paged_bounds", "dapq_paged_select", "dapq_paged_select_workspace_bytes", "dapq_paged_sparse_attention", "dapq_paged_sparse_attention_workspace_bytes",
 )
 
 
@@ -80,6 +81,14 @@ class Step(C.Structure):
     ]
 
 
+class Blocks(C.Structure):
+    """Mirror of `dapq_blocks`."""
+    _fields_ = [
+        ("block_rows", C.c_int32), ("n_select", C.c_int32), ("n_first", C.c_int32), ("n_last", C.c_int32),
+        ("bounds", C.c_void_p), ("scales", C.c_void_p),
+    ]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -123,19 +132,26 @@ def load_library():
     lib.dapq_paged_read.argtypes = [pp, vp, i32, vp, vp, vp]
     lib.dapq_paged_attention.argtypes = [pp, tp, vp, vp, vp, sz, vp]
     lib.dapq_paged_attention_workspace_bytes.argtypes = [pp, tp]
+    bp = C.POINTER(Blocks)
+    lib.dapq_paged_bounds.argtypes = [pp, bp, vp, vp, i32, vp]
+    lib.dapq_paged_select.argtypes = [pp, bp, tp, vp, vp, vp, vp, sz, vp]
+    lib.dapq_paged_select_workspace_bytes.argtypes = [pp, bp, tp]
+    lib.dapq_paged_sparse_attention.argtypes = [pp, bp, tp, vp, vp, vp, vp, vp, sz, vp]
+    lib.dapq_paged_sparse_attention_workspace_bytes.argtypes = [pp, bp, tp]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = C.c_int
     lib.dapq_pseudo_queries_workspace_bytes.restype = sz
     lib.dapq_score_static_capacity.restype = sz
     lib.dapq_topk_workspace_bytes.restype = sz
-    lib.dapq_paged_attention_workspace_bytes.restype = sz
+    for name in ("attention", "select", "sparse_attention"):
+        getattr(lib, f"dapq_paged_{name}_workspace_bytes").restype = sz
     try:
         from . import _native as native
     except ImportError as e:
         raise ImportError(f"the extension module {_PKG}/_native is not built for this Python; run "
                           "`python -m paper_2603_11564_amd.build` (there is no fallback path)") from e
     native.bind({name: C.cast(getattr(lib, name), vp).value for name in EXPORTS}, _resolve_current_stream, Shape, Qproj,
-                Pages, Step, _through_ctypes)
+                Pages, Step, Blocks, _through_ctypes)
     _native = native
     _lib = lib
     return lib
@@ -364,4 +380,37 @@ def paged_attention_workspace_bytes(pages, step) -> int:
 
 def dapq_paged_attention(pages, step, q, out, workspace, stream=None):
     if rc := (_native or _calls()).paged_attention(pages, step, q, out, workspace, stream):
+        _check(rc)
+
+
+def make_blocks(*, block_rows, n_select=1, n_first=0, n_last=1, bounds=None, scales=None) -> Blocks:
+    """bounds: device int8 [layers][n_pages][kv heads][page_rows / block_rows][2][128]; scales: uint8, the same without the last two.  The descriptor
+    keeps them alive; dapq_paged_sparse_attention needs neither."""
+    b = Blocks()
+    b.block_rows, b.n_select, b.n_first, b.n_last = block_rows, n_select, n_first, n_last
+    b.bounds, b.scales = _ptr(bounds), _ptr(scales)
+    b._keepalive = (bounds, scales)
+    return b
+
+
+def dapq_paged_bounds(pages, blocks, first, lengths, max_rows, stream=None):
+    if rc := (_native or _calls()).paged_bounds(pages, blocks, first, lengths, max_rows, stream):
+        _check(rc)
+
+
+def paged_select_workspace_bytes(pages, blocks, step) -> int:
+    return int(load_library().dapq_paged_select_workspace_bytes(C.byref(pages), C.byref(blocks), C.byref(step)))
+
+
+def dapq_paged_select(pages, blocks, step, q, idx, count, workspace, stream=None):
+    if rc := (_native or _calls()).paged_select(pages, blocks, step, q, idx, count, workspace, stream):
+        _check(rc)
+
+
+def paged_sparse_attention_workspace_bytes(pages, blocks, step) -> int:
+    return int(load_library().dapq_paged_sparse_attention_workspace_bytes(C.byref(pages), C.byref(blocks), C.byref(step)))
+
+
+def dapq_paged_sparse_attention(pages, blocks, step, q, idx, count, out, workspace, stream=None):
+    if rc := (_native or _calls()).paged_sparse_attention(pages, blocks, step, q, idx, count, out, workspace, stream):
         _check(rc)

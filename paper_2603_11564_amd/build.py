@@ -19,7 +19,8 @@ CEILING_LIB = os.path.join(PKG, "libdapq_ceiling.so")
 CEILING_SOURCES = ["ceiling.hip"]
 # (with the name of this Python's binary interface: another Python does not load it, and says so)
 NATIVE_LIB = os.path.join(PKG, "_native" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = ["common.hip", "rope.hip", "score.hip", "pool.hip", "topk.hip", "gather.hip", "recall.hip", "decode.hip", "qproj.hip", "paged.hip", "paged_attention.hip", "paged_turn.hip"]
+SOURCES = ["common.hip", "rope.hip", "score.hip", "pool.hip", "topk.hip", "gather.hip", "recall.hip", "decode.hip", "qproj.hip", "paged.hip", "paged_attention.hip", "paged_turn.hip",
+           "paged_blocks.hip", "paged_sparse.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
     # packed fp32 VALU forms are kept out of the generated code on purpose

@@ -14,7 +14,7 @@
 namespace {
 
 PyObject *g_resolver = nullptr, *g_stream = nullptr, *g_device = nullptr;  // see stream_of
-PyTypeObject *g_shape = nullptr, *g_qproj = nullptr, *g_pages = nullptr, *g_step = nullptr;  // the descriptors' classes
+PyTypeObject *g_shape = nullptr, *g_qproj = nullptr, *g_pages = nullptr, *g_step = nullptr, *g_blocks = nullptr;  // the descriptors' classes
 PyObject* g_other_way = nullptr;                                           // see other_way
 PyObject *g_data_ptr, *g_numel, *g_element_size, *g_cuda_stream;           // interned names
 
@@ -94,6 +94,7 @@ PyTypeObject* class_of(const dapq_shape*) { return g_shape; }
 PyTypeObject* class_of(const dapq_qproj*) { return g_qproj; }
 PyTypeObject* class_of(const dapq_pages*) { return g_pages; }
 PyTypeObject* class_of(const dapq_step*) { return g_step; }
+PyTypeObject* class_of(const dapq_blocks*) { return g_blocks; }
 template <typename T>
 bool struct_of(PyObject* v, T* out) {
   if (class_of(out) == nullptr || !PyObject_TypeCheck(v, class_of(out))) {
@@ -134,19 +135,22 @@ struct Calls {
   decltype(&dapq_paged_append) paged_append;
   decltype(&dapq_paged_read) paged_read;
   decltype(&dapq_paged_attention) paged_attention;
+  decltype(&dapq_paged_bounds) paged_bounds;
+  decltype(&dapq_paged_select) paged_select;
+  decltype(&dapq_paged_sparse_attention) paged_sparse_attention;
 };
 const char* const kNames[] = {"dapq_rope_apply", "dapq_score", "dapq_score_static", "dapq_score_stats", "dapq_score_accumulate",
                               "dapq_score_stats_extend", "dapq_pool", "dapq_topk", "dapq_pool_topk", "dapq_gather", "dapq_recall",
                               "dapq_decode_attention", "dapq_pseudo_tokens", "dapq_pseudo_queries", "dapq_paged_gather", "dapq_paged_append",
-                              "dapq_paged_read", "dapq_paged_attention"};
+                              "dapq_paged_read", "dapq_paged_attention", "dapq_paged_bounds", "dapq_paged_select", "dapq_paged_sparse_attention"};
 constexpr int kCalls = (int)(sizeof(kNames) / sizeof(kNames[0]));
 static_assert(sizeof(Calls) == kCalls * sizeof(void*), "a name for every function");
 Calls g_calls = {};
 
-// (addresses by name, resolver of the current stream, Shape, Qproj, Pages, Step, the way through ctypes)
+// (addresses by name, resolver of the current stream, Shape, Qproj, Pages, Step, Blocks, the way through ctypes)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!count_is(n, 7)) return nullptr;
-  for (int i = 2; i < 6; ++i)
+  if (!count_is(n, 8)) return nullptr;
+  for (int i = 2; i < 7; ++i)
     if (!PyType_Check(a[i])) return PyErr_Format(PyExc_TypeError, "classes expected");
   void* at[kCalls];
   for (int i = 0; i < kCalls; ++i) {
@@ -158,13 +162,13 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   __builtin_memcpy(&g_calls, at, sizeof(at));
   Py_INCREF(a[1]);
   Py_XSETREF(g_resolver, a[1]);
-  PyTypeObject** const classes[] = {&g_shape, &g_qproj, &g_pages, &g_step};
-  for (int i = 0; i < 4; ++i) {
+  PyTypeObject** const classes[] = {&g_shape, &g_qproj, &g_pages, &g_step, &g_blocks};
+  for (int i = 0; i < 5; ++i) {
     Py_INCREF(a[2 + i]);
     Py_XSETREF(*classes[i], reinterpret_cast<PyTypeObject*>(a[2 + i]));
   }
-  Py_INCREF(a[6]);
-  Py_XSETREF(g_other_way, a[6]);
+  Py_INCREF(a[7]);
+  Py_XSETREF(g_other_way, a[7]);
   Py_CLEAR(g_stream);
   Py_CLEAR(g_device);
   Py_RETURN_NONE;
@@ -342,11 +346,39 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return without_lock([&] { return g_calls.paged_attention(&g, &t, p[2], p[3], p[4], bytes, p[5]); });
 }
 
+PyObject* paged_bounds(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ARGS(6);
+  dapq_pages g;
+  dapq_blocks b;
+  if (!(struct_of(a[0], &g) && struct_of(a[1], &b) && P(2) && P(3) && I(4) && stream_of(a[5], &p[5]))) return other_way("dapq_paged_bounds", a, n);
+  return without_lock([&] { return g_calls.paged_bounds(&g, &b, IP(2), IP(3), I32(4), p[5]); });
+}
+PyObject* paged_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ARGS(8);
+  dapq_pages g;
+  dapq_blocks b;
+  dapq_step t;
+  size_t bytes;
+  if (!(struct_of(a[0], &g) && struct_of(a[1], &b) && struct_of(a[2], &t) && P(3) && P(4) && P(5) && P(6) && bytes_of(a[6], &bytes) && stream_of(a[7], &p[7])))
+    return other_way("dapq_paged_select", a, n);
+  return without_lock([&] { return g_calls.paged_select(&g, &b, &t, p[3], IP(4), IP(5), p[6], bytes, p[7]); });
+}
+PyObject* paged_sparse_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ARGS(9);
+  dapq_pages g;
+  dapq_blocks b;
+  dapq_step t;
+  size_t bytes;
+  if (!(struct_of(a[0], &g) && struct_of(a[1], &b) && struct_of(a[2], &t) && P(3) && P(4) && P(5) && P(6) && P(7) && bytes_of(a[7], &bytes) && stream_of(a[8], &p[8])))
+    return other_way("dapq_paged_sparse_attention", a, n);
+  return without_lock([&] { return g_calls.paged_sparse_attention(&g, &b, &t, p[3], IP(4), IP(5), p[6], p[7], bytes, p[8]); });
+}
+
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ENTRY(bind), ENTRY(rope_apply), ENTRY(score), ENTRY(score_static), ENTRY(score_stats), ENTRY(score_accumulate),
                           ENTRY(score_stats_extend), ENTRY(pool), ENTRY(topk), ENTRY(pool_topk), ENTRY(gather), ENTRY(recall),
                           ENTRY(decode_attention), ENTRY(pseudo_tokens), ENTRY(pseudo_queries), ENTRY(paged_gather), ENTRY(paged_append),
-                          ENTRY(paged_read), ENTRY(paged_attention), {nullptr, nullptr, 0, nullptr}};
+                          ENTRY(paged_read), ENTRY(paged_attention), ENTRY(paged_bounds), ENTRY(paged_select), ENTRY(paged_sparse_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "calls of libdapq with torch tensors", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

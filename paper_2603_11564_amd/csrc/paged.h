@@ -148,5 +148,34 @@ __device__ __forceinline__ unsigned larger_magnitude(unsigned x) {
   return a > b ? a : b;
 }
 
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp(unsigned x) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E;                               // lanes of a quad
+constexpr int kRor1 = 0x121, kRor2 = 0x122, kRor4 = 0x124, kRor8 = 0x128;  // of 16 lanes
+__device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
+
+// The sequence of token r and its number there, the same in all lanes; false if the token is none of a sequence's first max_new.
+__device__ __forceinline__ bool find_token(const int32_t* cu_new, int batch, int each_new, int max_new, int r, int lane, int* seq, int* t) {
+  if (cu_new == nullptr) {
+    *seq = r / each_new;
+    *t = r - *seq * each_new;
+  } else {
+    int before = 0, start = 0;  // sequences that end at or before r
+    for (int b0 = 0; b0 < batch; b0 += 64) {
+      const int end = b0 + lane < batch ? cu_new[b0 + lane + 1] : 0x7fffffff;
+      const int n = __popcll(__ballot(end <= r));
+      before += n;
+      if (n > 0) start = __shfl(end, n - 1, 64);
+      if (n < 64) break;
+    }
+    *seq = before;
+    *t = r - start;
+    if (before >= batch) return false;
+  }
+  return *t < max_new;
+}
+
 }  // namespace
 }  // namespace dapq

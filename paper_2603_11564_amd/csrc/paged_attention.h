@@ -32,6 +32,12 @@ inline int32_t most_new(const dapq_pages* pages, const dapq_step* step) {
 // 108.5 / 106.3, 64 of 1000 54.3 / 52.6; in 4 bits 16.3 / 14.6, 40.3 / 72.8, 45.4 / 74.0, 24.4 / 35.8.  4 columns: 11.8 / 13.4, 82.9 / 94.7, 97.9 / 100.6, 48.4 / 50.9; in 4 bits
 // 9.2 / 14.1, 31.3 / 70.6, 36.4 / 69.6, 14.6 / 34.4.
 constexpr int kMostRowCols = 32;
+// Checks that the calls of attention share, and the parameters of their kernels (host).
+int check_queries(const dapq_step* step);
+int check_attention(const dapq_pages* pages, const dapq_step* step);
+int check_buffers(const void* q, const void* out);
+int check_workspace(const void* workspace, size_t bytes, size_t need);
+PagedAttentionParams attention_params(const dapq_pages* pages, const dapq_step* step, const void* q, void* out, void* workspace);
 size_t turn_workspace_bytes(const dapq_pages* pages, const dapq_step* step);
 int launch_turn(const dapq_pages* pages, const dapq_step* step, const PagedAttentionParams& p, hipStream_t stream);
 
