@@ -116,195 +116,461 @@ struct SelectParams {
   int32_t batch, total_new, each_new, max_new, group, items;  // items: layers * Hkv
   int32_t block_shift, n_select, n_first, n_last;
   int32_t chunk, chunks, cols_log2;  // tiles of 16 blocks of a workgroup; such chunks of a sequence; columns of a token, a power of two
-  float inv_items, inv_chunks;
+  int32_t col_tiles;                 // that a workgroup has in LDS
+  float inv_items;
 };
 
 __device__ __forceinline__ int blocks_seen(const SelectParams& p, int before, int t) {
-  const int64_t most = (int64_t)p.pool.max_pages << p.pool.page_shift, n = (int64_t)before + t + 1;
-  return (int)(((n < 0 ? 0 : (n < most ? n : most)) + (1 << p.block_shift) - 1) >> p.block_shift);
+  const int most = p.pool.max_pages << p.pool.page_shift, n = (before < 1 << 30 ? before : 1 << 30) + t + 1;  // (rows are below 2^30, tokens no more than 2^25)
+  return ((n < 0 ? 0 : (n < most ? n : most)) + (1 << p.block_shift) - 1) >> p.block_shift;
 }
 
-// Largest of the 2^log2 lanes that a lane stands among (up to 16).
-__device__ __forceinline__ float largest_of_lanes(float x, int log2) {
-  auto with = [&](float y) { return fmaxf(x, y); };
-  if (log2 >= 1) x = with(__uint_as_float(dpp<kXor1>(__float_as_uint(x))));
-  if (log2 >= 2) x = with(__uint_as_float(dpp<kXor2>(__float_as_uint(x))));
-  if (log2 >= 3) x = with(__shfl_xor(x, 4, 64));
-  if (log2 >= 4) x = with(__shfl_xor(x, 8, 64));
-  return x;
+// Four values, each the largest of the 2^log2 lanes that a lane stands among (up to 16).  Lanes that agree already are taken by mirrors of 8 and 16 lanes.
+constexpr int kMirror8 = 0x141, kMirror16 = 0x140;
+template <int CTRL>
+__device__ __forceinline__ void with_lanes(float (&x)[4]) {
+#pragma unroll
+  for (int v = 0; v < 4; ++v) x[v] = fmaxf(x[v], __uint_as_float(dpp<CTRL>(__float_as_uint(x[v]))));
 }
+__device__ __forceinline__ void largest_of_lanes(float (&x)[4], int log2) {
+  if (log2 == 0) return;
+  with_lanes<kXor1>(x);
+  if (log2 == 1) return;
+  with_lanes<kXor2>(x);
+  if (log2 == 2) return;
+  with_lanes<kMirror8>(x);
+  if (log2 == 3) return;
+  with_lanes<kMirror16>(x);
+}
+
+// What is kept of a token's keys: those above `least`, and of those equal to it the first `equal`.
+struct Cut {
+  unsigned least, equal;
+};
+
+// The bin that the want-th largest of 256 bins' entries lies in, the same in all lanes: its number, what of `want` falls to it, and its entries.
+struct Bin {
+  unsigned at, want, entries;
+};
+__device__ __forceinline__ Bin find_bin(const unsigned* bins, unsigned want, int lane) {
+  const u32x4 x = *reinterpret_cast<const u32x4*>(bins + 252 - 4 * lane);  // from the top
+  const unsigned own = x[0] + x[1] + x[2] + x[3], upto = wave_scan<OpAdd>(own);
+  const int l = __builtin_ctzll(__ballot(upto >= want));
+  unsigned rest = want - (unsigned)__builtin_amdgcn_readlane((int)(upto - own), l);
+  unsigned bin = 255u - 4u * l;
+#pragma unroll
+  for (int i = 3; i > 0; --i) {
+    const unsigned n = (unsigned)__builtin_amdgcn_readlane((int)x[i], l);
+    if (rest <= n) return {bin, rest, n};
+    rest -= n;
+    --bin;
+  }
+  return {bin, rest, (unsigned)__builtin_amdgcn_readlane((int)x[0], l)};
+}
+
+// The n_select largest keys of a token and KV head, of equal ones the first, in order.  A workgroup has the keys in registers, REGS times four in a
+// row to a thread.  The range that scores take is cut into 256 bins, then the bin that the last kept key lies in, until all of a bin is kept or it
+// is one key; every wave reads the bins by itself, so that a round is one barrier.
+template <int WAVES, int REGS>
+struct Choice {
+  static constexpr int kTurn = 256 * WAVES;  // keys that the workgroup takes at a time
+  static_assert(WAVES * REGS <= 64, "a lane for the sum of each");
+  struct Lds {
+    __attribute__((aligned(16))) unsigned bins[4][256];
+    unsigned range[WAVES][4];  // of a wave: least and largest key, keys, ends
+    unsigned sums[WAVES * REGS];
+  };
+  // k: this thread's keys kTurn * r + 4 * tid .. + 3; row: layer, token and head as idx has them
+  static __device__ __forceinline__ void run(const SelectParams& p, Lds& lds, u32x4 (&k)[REGS], int blocks, int64_t row) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (tid < 256) lds.bins[i][tid] = 0;
+    unsigned low = kEndBlock, high = 0, n = 0, ends = 0;
+#pragma unroll
+    for (int r = 0; r < REGS; ++r) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (kTurn * r + 4 * tid + j >= blocks) k[r][j] = kNoBlock;
+        const unsigned x = k[r][j];
+        n += x != kNoBlock;
+        ends += x == kEndBlock;
+        low = x != kNoBlock && x < low ? x : low;
+        high = x != kEndBlock && x > high ? x : high;
+      }
+    }
+    low = wave_reduce<OpMin>(low);
+    high = wave_reduce<OpMax>(high);
+    n = wave_sum(n | ends << 16);  // (of a wave no more than 64 x 4 x REGS)
+    if (lane == 0) {
+      lds.range[wave][0] = low;
+      lds.range[wave][1] = high;
+      lds.range[wave][2] = n & 0xffffu;
+      lds.range[wave][3] = n >> 16;
+    }
+    __syncthreads();
+    n = ends = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      low = low < lds.range[w][0] ? low : lds.range[w][0];
+      high = larger(high, lds.range[w][1]);
+      n += lds.range[w][2];
+      ends += lds.range[w][3];
+    }
+    low = (unsigned)uniform((int)low), high = (unsigned)uniform((int)high);
+    Cut cut = {kNoBlock, 0};  // all
+    if (n > (unsigned)p.n_select) {
+      unsigned want = (unsigned)p.n_select - (unsigned)uniform((int)ends);
+      if (want == 0) {
+        cut.least = kEndBlock - 1;
+      } else {
+        // keys from `low` on, below low + 2^bits, in bins of 2^shift
+        int shift = high - low < 256u ? 0 : 24 - __builtin_clz(high - low);
+        int bits = 32;
+        for (int round = 0;; ++round) {
+#pragma unroll
+          for (int r = 0; r < REGS; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const unsigned x = k[r][j] - low;
+              if (k[r][j] != kNoBlock && k[r][j] != kEndBlock && k[r][j] >= low && (bits == 32 || x >> bits == 0)) atomicAdd(&lds.bins[round][x >> shift], 1u);
+            }
+          __syncthreads();
+          const Bin bin = find_bin(lds.bins[round], want, lane);
+          low += bin.at << shift;
+          want = bin.want;
+          if (bin.entries == want) {  // the whole bin
+            cut = {low - 1, 0};
+            break;
+          }
+          if (shift == 0) {
+            cut = {low, want};
+            break;
+          }
+          bits = shift;
+          shift = shift > 8 ? shift - 8 : 0;
+        }
+      }
+    }
+    // in order, before a thread's keys: above the cut in the low half, equal to it in the high one
+    unsigned upto[REGS];
+#pragma unroll
+    for (int r = 0; r < REGS; ++r) {
+      unsigned both = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) both += (unsigned)(k[r][j] > cut.least) + ((unsigned)(k[r][j] == cut.least && k[r][j] != kNoBlock) << 16);
+      upto[r] = wave_scan<OpAdd>(both);
+      if (lane == 63) lds.sums[WAVES * r + wave] = upto[r];
+      upto[r] -= both;
+    }
+    __syncthreads();
+    const unsigned sum = lane < WAVES * REGS ? lds.sums[lane] : 0, before = wave_scan<OpAdd>(sum);
+    int32_t* out = p.idx + row * p.n_select;
+#pragma unroll
+    for (int r = 0; r < REGS; ++r) {
+      unsigned here = upto[r] + (unsigned)__builtin_amdgcn_readlane((int)(before - sum), WAVES * r + wave);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const unsigned above = here & 0xffffu, equal = here >> 16;
+        const bool same = k[r][j] == cut.least && k[r][j] != kNoBlock;
+        if (k[r][j] > cut.least || (same && equal < cut.equal)) out[above + (equal < cut.equal ? equal : cut.equal)] = kTurn * r + 4 * tid + j;
+        here += (unsigned)(k[r][j] > cut.least) + ((unsigned)same << 16);
+      }
+    }
+    if (tid == 0) {
+      const unsigned all = (unsigned)__builtin_amdgcn_readlane((int)before, 63);
+      p.count[row] = (int)((all & 0xffffu) + (all >> 16 < cut.equal ? all >> 16 : cut.equal));
+    }
+  }
+};
+
+constexpr int kColTiles = 8, kColTileBytes = 4096;  // column tiles in LDS, at most; u+ and u- of 16 columns
 
 // The score is a product of whole numbers of 8 bits, 256 long: with u+ = max(u, 0) and u- = min(u, 0), max(u * upper, u * lower) = u+ * upper + u- * lower.
 // D[block][column] = bounds (A, 16 blocks) x (u+, u-) (B, 16 columns: query heads of a token, padded to a power of two) on v_mfma_i32_16x16x64_i8, exact.
-// Bound by the bytes of the bounds.  A wave has a tile of 16 blocks at a time.
-__global__ __launch_bounds__(256) void paged_scores_kernel(SelectParams p) {
+// Bound by the bytes of the bounds.  A workgroup brings the columns of some tokens into LDS as operands, then each wave takes tiles of 16 blocks.
+// COLUMNS: kOne: one column tile in all, whose operand stays in registers; kMany; kWide: a token has more than 16 query heads, and several column tiles.
+// REGS: of the Choice of the same workgroup, which has all tiles of the sequence and keeps their keys in LDS; 0: the keys go to the workspace.
+enum Columns { kOne, kMany, kWide };
+constexpr int kScoreWaves = 4, kWholeWaves = 8;
+template <int COLUMNS, int REGS>
+__global__ __launch_bounds__(64 * (REGS > 0 ? kWholeWaves : kScoreWaves)) void paged_scores_kernel(SelectParams p) {
   touch_args<sizeof(SelectParams)>();
-  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
-  const int wave = uniform(threadIdx.x >> 6);
-  const int of_item = uniform_quotient(blockIdx.x, p.chunks, p.inv_chunks), chunk = blockIdx.x - of_item * p.chunks;
+  constexpr bool WIDE = COLUMNS == kWide, WHOLE = REGS > 0;
+  constexpr int WAVES = WHOLE ? kWholeWaves : kScoreWaves;
+  extern __shared__ char lds[];  // column tiles; the units of their columns; WHOLE: keys
+  float* units = reinterpret_cast<float*>(lds + p.col_tiles * kColTileBytes);
+  unsigned* whole_keys = reinterpret_cast<unsigned*>(units + 16 * p.col_tiles);
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kg = lane >> 4;
+  const int wave = uniform(tid >> 6);
+  // (chunks of the same number follow each other: workgroups go round the chip's eight parts, and late chunks are those that sequences do not have)
+  const int all_items = p.items * p.batch, chunk = blockIdx.x / all_items, of_item = blockIdx.x - chunk * all_items;
   const int seq = uniform_quotient(of_item, p.items, p.inv_items), item = of_item - seq * p.items;
   const int layer = item / p.pool.n_kv_heads, head = item - layer * p.pool.n_kv_heads;
+  // the pages of the first tile are on their way before it is known whether there is one
+  const int32_t* table = p.pool.table + (int64_t)seq * p.pool.max_pages;
+  const int to_page = p.pool.page_shift - p.block_shift;  // blocks of a page, log2
+  auto page_of = [&](int k) {
+    const int e = (16 * k + n) >> to_page;
+    return table[e < p.pool.max_pages ? e : p.pool.max_pages - 1];
+  };
+  int page = page_of(chunk * p.chunk + wave);
   const int first = uniform(p.cu_new == nullptr ? seq * p.each_new : p.cu_new[seq]);
   int tokens = p.cu_new == nullptr ? p.each_new : uniform(p.cu_new[seq + 1]) - first;
   tokens = tokens < p.max_new ? tokens : p.max_new;
   if (tokens <= 0) return;
   const int before = uniform(p.lengths[seq]);
   const int tiles = (blocks_seen(p, before, tokens - 1) + 15) >> 4, tile0 = chunk * p.chunk, tile1 = tile0 + p.chunk < tiles ? tile0 + p.chunk : tiles;
-  if (tile0 >= tile1) return;
-  const int wide = p.cols_log2 > 4 ? p.cols_log2 - 4 : 0;  // a token has 2^wide column tiles
-  const int each = p.cols_log2 < 4 ? 4 - p.cols_log2 : 0;  // or a column tile 2^each tokens
-  for (int64_t t0 = (int64_t)blockIdx.y << each; t0 < tokens; t0 += (int64_t)gridDim.y << each) {
-    const int token = (int)t0 + (n >> p.cols_log2);
-    const int seen = token < tokens ? blocks_seen(p, before, token) : 0;
-    for (int k0 = tile0 + wave; k0 < tile1; k0 += 4) {
-      const int64_t row = (int64_t)(16 * k0 + n) << p.block_shift;
-      const int64_t at = row >> p.pool.page_shift < p.pool.max_pages ? find_row(p.pool, layer, seq, head, row) >> p.block_shift : -1;
-      i32x4 a[4];
-      const uint8_t* src = p.bounds + (at < 0 ? 0 : at) * (2 * kHeadDim) + 16 * kg;
+  if (!WHOLE && tile0 >= tile1) return;
+  // A tile is asked for while the one before it is used, its pages one tile earlier.
+  struct Tile {
+    i32x4 a[4];
+    int scale;  // -1 on no page
+  };
+  const int64_t head_of_layer = ((int64_t)layer * p.pool.n_pages * p.pool.n_kv_heads + head) << to_page;
+  auto fetch = [&](Tile& tile, int k, int page) {
+    const int block = 16 * k + n;
+    const bool there = k < tile1 && page >= 0 && page < p.pool.n_pages && block >> to_page < p.pool.max_pages;
+    const int64_t at = there ? head_of_layer + (((int64_t)page * p.pool.n_kv_heads) << to_page) + (block & ((1 << to_page) - 1)) : 0;
+    const uint8_t* src = p.bounds + at * (2 * kHeadDim) + 16 * kg;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = at < 0 ? i32x4{0, 0, 0, 0} : *reinterpret_cast<const i32x4*>(src + 64 * i);
-      const int scale = at < 0 ? -1 : p.scales[at];
-      float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      for (int w = 0; w < 1 << wide; ++w) {
-        const int col = wide ? 16 * w + n : n & ((1 << p.cols_log2) - 1);
-        const bool real = token < tokens && col < p.group;
-        // the column's whole numbers: channels 16 * kg .. + 15 and 64 further on
-        const uint16_t* qs = p.q + layer * p.q_stride_layer + (int64_t)(first + (real ? token : 0)) * p.q_stride_row + (int64_t)(head * p.group + (real ? col : 0)) * p.q_stride_head;
-        u32x4 x[4];
-        unsigned largest = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[i] = *reinterpret_cast<const u32x4*>(qs + 64 * (i >> 1) + 16 * kg + 8 * (i & 1));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) largest = larger(largest, larger_magnitude(x[i][j]));
-        }
-        largest = larger(largest, (unsigned)__shfl_xor((int)largest, 16, 64));
-        largest = larger(largest, (unsigned)__shfl_xor((int)largest, 32, 64));
+    for (int i = 0; i < 4; ++i) tile.a[i] = *reinterpret_cast<const i32x4*>(src + 64 * i);
+    const int scale = p.scales[at];
+    tile.scale = there ? scale : -1;
+  };
+  const int log2 = WIDE ? 4 : p.cols_log2, each = 16 >> log2;  // tokens of a column tile
+  const int all = WIDE ? (p.group + 15) >> 4 : (tokens + each - 1) / each;  // column tiles: of a token, or of the sequence
+  const int middle0 = p.n_first, middle1 = blocks_seen(p, before, 0) - p.n_last;  // blocks that all tokens score
+  for (int64_t t0 = WIDE ? blockIdx.y : 0; t0 < (WIDE ? tokens : 1); t0 += gridDim.y) {
+    for (int c0 = WIDE ? 0 : blockIdx.y * p.col_tiles; c0 < all; c0 += WIDE ? p.col_tiles : (int)gridDim.y * p.col_tiles) {
+      const int here = COLUMNS == kOne ? 1 : (all - c0 < p.col_tiles ? all - c0 : p.col_tiles);
+      Tile even, odd;
+      if (t0 > blockIdx.y || c0 > 0) page = page_of(tile0 + wave);
+      // 16 lanes to a column, eight channels to a lane; columns that there are not are the last one that there is
+      const int col = tid >> 4 & 15, o = tid & 15;
+      auto query = [&](int c) {
+        c = c < here ? c : here - 1;
+        int token = WIDE ? (int)t0 : (c0 + c) * each + (col >> log2), h = WIDE ? (c0 + c) * 16 + col : col & ((1 << log2) - 1);
+        token = token < tokens ? token : tokens - 1;
+        h = head * p.group + (h < p.group ? h : p.group - 1);
+        return *reinterpret_cast<const u32x4*>(p.q + layer * p.q_stride_layer + (int64_t)(first + token) * p.q_stride_row + (int64_t)h * p.q_stride_head + 8 * o);
+      };
+      u32x4 x = query(tid >> 8);
+      fetch(even, tile0 + wave, page);
+      page = page_of(tile0 + wave + WAVES);
+      for (int c = tid >> 8; c < here; c += WAVES / 4) {
+        if (c >= WAVES / 4) x = query(c);
+        unsigned largest = larger(larger(larger_magnitude(x[0]), larger_magnitude(x[1])), larger(larger_magnitude(x[2]), larger_magnitude(x[3])));
+        largest = larger(largest, dpp<kRor1>(largest));
+        largest = larger(largest, dpp<kRor2>(largest));
+        largest = larger(largest, dpp<kRor4>(largest));
+        largest = larger(largest, dpp<kRor8>(largest));
         const bool bad = largest >= 0x7f80u;
         const int unit = unit_byte(bad ? 0 : largest);
         const float per = power_of_two(254 - unit);
-        i32x4 d = {0, 0, 0, 0};
-        i32x4 up[2], down[2];
+        u32x2 up = {0, 0}, down = {0, 0};
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int e = 0; e < 8; ++e) {
+          const unsigned two = x[e >> 1];
+          const float f = __uint_as_float(e & 1 ? two & 0xffff0000u : two << 16);
+          const int whole = bad ? 0 : (int)rintf(fminf(fmaxf(f * per, -127.0f), 127.0f));
+          up[e >> 2] |= (unsigned)(whole > 0 ? whole : 0) << (8 * (e & 3));
+          down[e >> 2] |= ((unsigned)(whole < 0 ? whole : 0) & 255u) << (8 * (e & 3));
+        }
+        char* at = lds + c * kColTileBytes + (((o >> 3) * 64 + (o >> 1 & 3) * 16 + col) * 16 + (o & 1) * 8);
+        *reinterpret_cast<u32x2*>(at) = up;
+        *reinterpret_cast<u32x2*>(at + 2048) = down;
+        if (o == 0) units[c * 16 + col] = power_of_two(unit);
+      }
+      __syncthreads();
+      i32x4 own[4];  // kOne: the column tile's operand
+      float own_unit = 0.0f;
+      auto operand = [&](int c, int i) { return reinterpret_cast<const i32x4*>(lds + c * kColTileBytes)[64 * i + lane]; };
+      if constexpr (COLUMNS == kOne) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            unsigned u = 0, v = 0;
+        for (int i = 0; i < 4; ++i) own[i] = operand(0, i);
+        own_unit = units[n];
+      }
+      // where the keys of this lane's token, in the first column tile here, are written; of the next one `next` further on
+      const int token0 = WIDE ? (int)t0 : c0 * each + (n >> log2);
+      const int64_t next = WHOLE ? each * p.stride : (int64_t)each * p.pool.n_kv_heads * p.stride;
+      unsigned* const to0 = (WHOLE ? whole_keys + token0 * p.stride : p.keys + (((int64_t)layer * p.total_new + first + token0) * p.pool.n_kv_heads + head) * p.stride) + 4 * kg;
+      const bool writes = (n & ((1 << log2) - 1)) == 0;
+      auto use = [&](const Tile& tile, int k) {
+        const bool plain = 16 * k >= middle0 && 16 * k + 16 <= middle1 && !__any(tile.scale < 0 || tile.scale == 255);
+        float factor[4];  // of this lane's blocks
+        const float mine = power_of_two(tile.scale < 0 ? 0 : tile.scale);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const unsigned two = x[2 * i + (j >> 1)][2 * (j & 1) + (e >> 1)];
-              const float f = __uint_as_float(e & 1 ? two & 0xffff0000u : two << 16);
-              const int whole = bad ? 0 : (int)rintf(fminf(fmaxf(f * per, -127.0f), 127.0f));
-              u |= (unsigned)(whole > 0 ? whole : 0) << (8 * e);
-              v |= ((unsigned)(whole < 0 ? whole : 0) & 255u) << (8 * e);
+        for (int v = 0; v < 4; ++v) factor[v] = __shfl(mine, 4 * kg + v, 64);
+        auto put = [&](float (&best)[4], int c) {
+          const int token = WIDE ? token0 : token0 + c * each;
+          u32x4 keys;
+          largest_of_lanes(best, log2);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) keys[v] = key_of(best[v] * factor[v]);
+          if (!plain) {
+            const int seen = blocks_seen(p, before, token);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int block = 16 * k + 4 * kg + v, s = __shfl(tile.scale, 4 * kg + v, 64);
+              if (s == 255) keys[v] = kBadBlock;
+              if (block < p.n_first || block >= seen - p.n_last) keys[v] = kEndBlock;
+              if (block >= seen || s < 0) keys[v] = kNoBlock;
             }
-            up[i][j] = (int)u;
-            down[i][j] = (int)v;
           }
+          u32x4* to = reinterpret_cast<u32x4*>(to0 + (WIDE ? 0 : c * next) + 16 * k);
+          if (writes && token < tokens) {
+            if (WIDE && c0 > 0) {  // (what this lane has written for the query heads before these)
+              const u32x4 old = *to;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) d = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], up[i], d, 0, 0, 0);
+              for (int v = 0; v < 4; ++v) keys[v] = larger(keys[v], old[v]);
+            }
+            *to = keys;
+          }
+        };
+        float of_token[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 2
+        for (int c = 0; c < here; ++c) {
+          i32x4 up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 2; ++i) d = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[2 + i], down[i], d, 0, 0, 0);
-        const float two_to_f = power_of_two(unit);
+          for (int i = 0; i < 2; ++i) {
+            up = __builtin_amdgcn_mfma_i32_16x16x64_i8(tile.a[i], COLUMNS == kOne ? own[i] : operand(c, i), up, 0, 0, 0);
+            down = __builtin_amdgcn_mfma_i32_16x16x64_i8(tile.a[2 + i], COLUMNS == kOne ? own[2 + i] : operand(c, 2 + i), down, 0, 0, 0);
+          }
+          const float unit = COLUMNS == kOne ? own_unit : units[c * 16 + n];
+          float best[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) best[v] = fmaxf(best[v], real ? (float)d[v] * two_to_f : -INFINITY);
+          for (int v = 0; v < 4; ++v) {
+            best[v] = (float)(up[v] + down[v]) * unit;
+            of_token[v] = fmaxf(of_token[v], best[v]);
+          }
+          if (!WIDE) put(best, c);
+        }
+        if (WIDE) put(of_token, 0);
+      };
+      for (int k = tile0 + wave; k < tile1; k += 2 * WAVES) {
+        fetch(odd, k + WAVES, page);
+        page = page_of(k + 2 * WAVES);
+        use(even, k);
+        fetch(even, k + 2 * WAVES, page);
+        page = page_of(k + 3 * WAVES);
+        if (k + WAVES < tile1) use(odd, k + WAVES);
       }
-      u32x4 keys;
+      if (WHOLE || COLUMNS != kOne) __syncthreads();
+    }
+  }
+  if constexpr (WHOLE) {
+    using C = Choice<WAVES, REGS>;
+    __shared__ typename C::Lds choice;
+    for (int t = 0; t < tokens; ++t) {
+      const unsigned* keys = whole_keys + t * p.stride;
+      const int blocks = blocks_seen(p, before, t);
+      u32x4 k[REGS];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const float top = largest_of_lanes(best[v], p.cols_log2);
-        const int block = 16 * k0 + 4 * kg + v, s = __shfl(scale, 4 * kg + v, 64);
-        const unsigned scored = s == 255 ? kBadBlock : key_of(top * power_of_two(s < 0 ? 0 : s));
-        keys[v] = block >= seen || s < 0 ? kNoBlock : (block < p.n_first || block >= seen - p.n_last ? kEndBlock : scored);
-      }
-      if (token < tokens && (n & ((1 << (p.cols_log2 < 4 ? p.cols_log2 : 4)) - 1)) == 0)
-        *reinterpret_cast<u32x4*>(p.keys + (((int64_t)layer * p.total_new + first + token) * p.pool.n_kv_heads + head) * p.stride + 16 * k0 + 4 * kg) = keys;
+      for (int r = 0; r < REGS; ++r) k[r] = C::kTurn * r + 4 * tid < blocks ? *reinterpret_cast<const u32x4*>(keys + C::kTurn * r + 4 * tid) : u32x4{0, 0, 0, 0};
+      C::run(p, choice, k, blocks, ((int64_t)layer * p.total_new + first + t) * p.pool.n_kv_heads + head);
     }
   }
 }
 
-// The n_select largest keys of a token and KV head, of equal ones the first: a workgroup finds the smallest key that is kept, eight bits at a time, then
-// writes down in order what lies above it and as many of its like as there is room for.
-__global__ __launch_bounds__(256) void paged_choose_kernel(SelectParams p) {
+template <int WAVES, int REGS>
+__global__ __launch_bounds__(64 * WAVES) void paged_choose_kernel(SelectParams p) {
   touch_args<sizeof(SelectParams)>();
-  __shared__ unsigned bins[256];
-  __shared__ unsigned found[2];
-  __shared__ unsigned wave_sums[4];
+  using C = Choice<WAVES, REGS>;
+  __shared__ typename C::Lds lds;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int row = blockIdx.x / p.pool.n_kv_heads;  // layer * total_new + token
+  const unsigned* keys = p.keys + (int64_t)blockIdx.x * p.stride;
+  u32x4 k[REGS];
+  auto load = [&](int r, int end) { k[r] = C::kTurn * r + 4 * tid < end ? *reinterpret_cast<const u32x4*>(keys + C::kTurn * r + 4 * tid) : u32x4{0, 0, 0, 0}; };
+  constexpr bool kEarly = WAVES * REGS <= 8;  // (the few keys of a narrow table are on their way before it is known how many of them count)
+  if constexpr (kEarly)
+#pragma unroll
+    for (int r = 0; r < REGS; ++r) load(r, (int)p.stride);
+  int seq, t;
+  if (!find_token(p.cu_new, p.batch, p.each_new, p.max_new, row % p.total_new, lane, &seq, &t)) return;
+  const int blocks = uniform(blocks_seen(p, p.lengths[seq], t));
+  if constexpr (!kEarly)
+#pragma unroll
+    for (int r = 0; r < REGS; ++r) load(r, blocks);  // (a row has room for whole tiles)
+  C::run(p, lds, k, blocks, blockIdx.x);
+}
+
+// The same of any number of keys, read again from memory for every eight bits of the smallest one that is kept.
+__global__ __launch_bounds__(256) void paged_choose_long_kernel(SelectParams p) {
+  touch_args<sizeof(SelectParams)>();
+  __shared__ __attribute__((aligned(16))) unsigned bins[4][256];
+  __shared__ unsigned sums[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int row = blockIdx.x / p.pool.n_kv_heads;  // layer * total_new + token
-  const int r = row % p.total_new;
   int seq, t;
-  if (!find_token(p.cu_new, p.batch, p.each_new, p.max_new, r, lane, &seq, &t)) return;
-  const int blocks = blocks_seen(p, uniform(p.lengths[seq]), t);
+  if (!find_token(p.cu_new, p.batch, p.each_new, p.max_new, row % p.total_new, lane, &seq, &t)) return;
+  const int blocks = uniform(blocks_seen(p, p.lengths[seq], t));
   const unsigned* keys = p.keys + (int64_t)blockIdx.x * p.stride;
-  unsigned least = 0, want = (unsigned)p.n_select;  // the kept keys' leading bits so far; how many of those with the same are kept
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    bins[tid] = 0;
-    __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bins[i][tid] = 0;
+  __syncthreads();
+  Cut cut = {0, 0};
+  unsigned want = (unsigned)p.n_select;
+  for (int round = 0; round < 4; ++round) {
+    const int shift = 24 - 8 * round;
     for (int i = tid; i < blocks; i += 256) {
       const unsigned k = keys[i];
-      if (k != kNoBlock && (shift == 24 || (k ^ least) >> (shift + 8) == 0)) atomicAdd(&bins[(k >> shift) & 255u], 1u);
+      if (k != kNoBlock && (round == 0 || (k ^ cut.least) >> (shift + 8) == 0)) atomicAdd(&bins[round][(k >> shift) & 255u], 1u);
     }
     __syncthreads();
-    // bins from the top: thread tid has bin 255 - tid
-    const unsigned mine = bins[255 - tid];
-    unsigned upto = wave_scan<OpAdd>(mine);
-    if (lane == 63) wave_sums[wave] = upto;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) upto += wave_sums[w];
-    if (tid == 255) found[0] = upto < want ? ~0u : 0u;  // (fewer keys than wanted: only in the first round)
-    __syncthreads();
-    if (found[0] == ~0u) {
-      least = kNoBlock;
-      want = 0;
-      break;
+    if (round == 0) {
+      unsigned all = bins[0][4 * lane] + bins[0][4 * lane + 1] + bins[0][4 * lane + 2] + bins[0][4 * lane + 3];
+      all = wave_sum(all);
+      if (all <= want) {  // (the same in all waves)
+        want = 0;
+        break;
+      }
     }
-    if (upto >= want && upto - mine < want) found[1] = (unsigned)(255 - tid), found[0] = want - (upto - mine);
-    __syncthreads();
-    least |= found[1] << shift;
-    want = found[0];
-    __syncthreads();
+    const Bin bin = find_bin(bins[round], want, lane);
+    cut.least |= bin.at << shift;
+    want = bin.want;
   }
-  // `want` of the keys equal to `least` (none of the keys of no block), and all above
+  cut.equal = want;
   int32_t* out = p.idx + (int64_t)blockIdx.x * p.n_select;
   unsigned above = 0, equal = 0;  // so far
-  for (int i0 = 0; i0 < blocks; i0 += 1024) {
+  for (int i0 = 0, turn = 0; i0 < blocks; i0 += 1024, turn ^= 1) {
     unsigned k[4];
-    unsigned a = 0, e = 0;
+    unsigned both = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int i = i0 + 4 * tid + j;
       k[j] = i < blocks ? keys[i] : kNoBlock;
-      a += k[j] > least;
-      e += k[j] == least;
+      both += (unsigned)(k[j] > cut.least) + ((unsigned)(k[j] == cut.least) << 16);
     }
-    const unsigned both = a | e << 16;
-    unsigned upto = wave_scan<OpAdd>(both);
-    __syncthreads();
-    if (lane == 63) wave_sums[wave] = upto;
-    __syncthreads();
-    unsigned all = 0;
+    const unsigned upto = wave_scan<OpAdd>(both);
+    if (lane == 63) sums[turn][wave] = upto;
+    __syncthreads();  // (the sums of the turn before last are overwritten behind it)
+    unsigned all = 0, before = upto - both;
+#pragma unroll
     for (int w = 0; w < 4; ++w) {
-      if (w < wave) upto += wave_sums[w];
-      all += wave_sums[w];
+      before += w < wave ? sums[turn][w] : 0;
+      all += sums[turn][w];
     }
-    unsigned a0 = above + ((upto - both) & 0xffffu), e0 = equal + ((upto - both) >> 16);
+    unsigned a = above + (before & 0xffffu), e = equal + (before >> 16);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool take = k[j] > least || (k[j] == least && e0 < want);
-      if (take) out[a0 + (e0 < want ? e0 : want)] = i0 + 4 * tid + j;
-      a0 += k[j] > least;
-      e0 += k[j] == least;
+      if (k[j] > cut.least || (k[j] == cut.least && e < cut.equal)) out[a + (e < cut.equal ? e : cut.equal)] = i0 + 4 * tid + j;
+      a += k[j] > cut.least;
+      e += k[j] == cut.least;
     }
     above += all & 0xffffu;
     equal += all >> 16;
   }
-  if (tid == 0) p.count[blockIdx.x] = (int)(above + (equal < want ? equal : want));
+  if (tid == 0) p.count[blockIdx.x] = (int)(above + (equal < cut.equal ? equal : cut.equal));
 }
 
+constexpr int kWholeKeys = 64 << 10;  // bytes of keys in LDS, at most
 struct SelectPlan {
-  int64_t stride, chunk, chunks, col_tiles;
-  int cols_log2;
+  int64_t stride, chunk, chunks, columns;  // columns: workgroups along the column tiles
+  int cols_log2, col_tiles;
+  bool whole;  // a workgroup scores all blocks of a sequence and KV head and chooses them
+  int lds;
 };
 SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step) {
   SelectPlan plan;
@@ -313,12 +579,22 @@ SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
   const int group = step->n_q_heads / pages->n_kv_heads;
   plan.cols_log2 = 0;
   while (1 << plan.cols_log2 < group) ++plan.cols_log2;
-  const int64_t each = plan.cols_log2 < 4 ? 16 >> plan.cols_log2 : 1;
-  plan.col_tiles = (most_new(pages, step) + each - 1) / each;
-  if (plan.col_tiles > 65535) plan.col_tiles = 65535;
+  const int64_t most = most_new(pages, step), each = plan.cols_log2 < 4 ? 16 >> plan.cols_log2 : 1;
+  const int64_t tiles_of_columns = plan.cols_log2 > 4 ? (group + 15) / 16 : (most + each - 1) / each;
+  plan.col_tiles = (int)(tiles_of_columns < kColTiles ? (tiles_of_columns < 1 ? 1 : tiles_of_columns) : kColTiles);
+  plan.columns = plan.cols_log2 > 4 ? most : (tiles_of_columns + plan.col_tiles - 1) / plan.col_tiles;
+  plan.columns = plan.columns < 1 ? 1 : (plan.columns > 65535 ? 65535 : plan.columns);
   const int64_t items = (int64_t)pages->n_layers * pages->batch * pages->n_kv_heads;
-  plan.chunk = (tiles * items + 2047) / 2048;
-  plan.chunk = plan.chunk < 4 ? 4 : (plan.chunk + 3) / 4 * 4;
+  plan.lds = plan.col_tiles * (kColTileBytes + 64);
+  const int64_t key_bytes = most * plan.stride * 4;
+  plan.whole = plan.cols_log2 <= 4 && plan.columns == 1 && key_bytes <= kWholeKeys && plan.stride <= 8192 && items >= 128;
+  if (plan.whole) {
+    plan.lds += (int)key_bytes;
+    plan.chunk = tiles;
+  } else {
+    plan.chunk = (tiles * items + 2047) / 2048;
+    plan.chunk = plan.chunk < 4 ? 4 : (plan.chunk + 3) / 4 * 4;
+  }
   plan.chunks = (tiles + plan.chunk - 1) / plan.chunk;
   return plan;
 }
@@ -329,8 +605,9 @@ int check_select(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_
   if (rc == DAPQ_OK) rc = check_step(pages, step);
   if (rc == DAPQ_OK) rc = check_queries(step);
   if (rc != DAPQ_OK) return rc;
-  DAPQ_REQUIRE((int64_t)pages->n_layers * step->total_new * pages->n_kv_heads < (int64_t)1 << 24, DAPQ_ERR_UNSUPPORTED,
-               "n_layers * total_new * n_kv_heads (%lld) must be below 2^24", (long long)(pages->n_layers * step->total_new * pages->n_kv_heads));
+  // (a launch holds fewer than 2^32 threads along an axis)
+  DAPQ_REQUIRE((int64_t)pages->n_layers * step->total_new * pages->n_kv_heads < (int64_t)1 << 22, DAPQ_ERR_UNSUPPORTED,
+               "n_layers * total_new * n_kv_heads (%lld) must be below 2^22", (long long)(pages->n_layers * step->total_new * pages->n_kv_heads));
   DAPQ_REQUIRE(step->n_q_heads <= 65535, DAPQ_ERR_UNSUPPORTED, "n_q_heads (%d) exceeds 65535", step->n_q_heads);
   return DAPQ_OK;
 }
@@ -370,7 +647,8 @@ extern "C" DAPQ_API int dapq_paged_bounds(const dapq_pages* pages, const dapq_bl
 extern "C" DAPQ_API size_t dapq_paged_select_workspace_bytes(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step) {
   if (check_select(pages, blocks, step) != DAPQ_OK) return 0;
   const int64_t rows = (int64_t)pages->n_layers * step->total_new * pages->n_kv_heads;
-  return align_up((size_t)(rows < 1 ? 1 : rows) * select_plan(pages, blocks, step).stride * sizeof(unsigned), 256);
+  const SelectPlan plan = select_plan(pages, blocks, step);
+  return plan.whole ? 256 : align_up((size_t)(rows < 1 ? 1 : rows) * plan.stride * sizeof(unsigned), 256);
 }
 
 extern "C" DAPQ_API int dapq_paged_select(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, const void* q, int32_t* idx,
@@ -407,11 +685,26 @@ extern "C" DAPQ_API int dapq_paged_select(const dapq_pages* pages, const dapq_bl
   p.chunks = (int32_t)plan.chunks;
   p.cols_log2 = plan.cols_log2;
   p.inv_items = 1.0f / (float)p.items;
-  p.inv_chunks = 1.0f / (float)p.chunks;
-  hipLaunchKernelGGL(paged_scores_kernel, dim3((unsigned)((int64_t)p.items * p.batch * p.chunks), (unsigned)plan.col_tiles), dim3(256), 0,
-                     static_cast<hipStream_t>(stream), p);
+  p.col_tiles = plan.col_tiles;
+  const hipStream_t on = static_cast<hipStream_t>(stream);
+  const dim3 grid((unsigned)((int64_t)p.items * p.batch * p.chunks), (unsigned)plan.columns);
+  if (plan.whole) {
+    auto kernel = plan.col_tiles == 1 ? (plan.stride <= 2048 ? paged_scores_kernel<kOne, 1> : paged_scores_kernel<kOne, 4>)
+                                      : (plan.stride <= 2048 ? paged_scores_kernel<kMany, 1> : paged_scores_kernel<kMany, 4>);
+    rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), kColTiles * (kColTileBytes + 64) + kWholeKeys);
+    if (rc != DAPQ_OK) return rc;
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * kWholeWaves), plan.lds, on, p);
+    DAPQ_HIP_LAUNCH_CHECK("paged_scores_kernel");
+    return DAPQ_OK;
+  }
+  hipLaunchKernelGGL((plan.cols_log2 > 4 ? paged_scores_kernel<kWide, 0> : (plan.col_tiles == 1 ? paged_scores_kernel<kOne, 0> : paged_scores_kernel<kMany, 0>)),
+                     grid, dim3(64 * kScoreWaves), plan.lds, on, p);
   DAPQ_HIP_LAUNCH_CHECK("paged_scores_kernel");
-  hipLaunchKernelGGL(paged_choose_kernel, dim3((unsigned)((int64_t)p.items * p.total_new)), dim3(256), 0, static_cast<hipStream_t>(stream), p);
+  const unsigned rows = (unsigned)((int64_t)p.items * p.total_new);
+  if (plan.stride <= 1024) hipLaunchKernelGGL((paged_choose_kernel<4, 1>), dim3(rows), dim3(256), 0, on, p);
+  else if (plan.stride <= 2048) hipLaunchKernelGGL((paged_choose_kernel<4, 2>), dim3(rows), dim3(256), 0, on, p);
+  else if (plan.stride <= 16384) hipLaunchKernelGGL((paged_choose_kernel<16, 4>), dim3(rows), dim3(1024), 0, on, p);
+  else hipLaunchKernelGGL(paged_choose_long_kernel, dim3(rows), dim3(256), 0, on, p);
   DAPQ_HIP_LAUNCH_CHECK("paged_choose_kernel");
   return DAPQ_OK;
 }

@@ -76,7 +76,7 @@ REFUSED = [
     (lambda: select(work=At(0, 128)), ERR_WORKSPACE, "workspace has 128 bytes"), (lambda: select(s=step(q_strides=(0, 64, 128))), ERR_UNSUPPORTED, "q strides"),
     (lambda: select(s=step(q_strides=(0, 1024, 4))), ERR_UNSUPPORTED, "q strides"), (lambda: select(s=step(lengths=N)), ERR_INVALID, "lengths"),
     (lambda: select(s=step(n_q_heads=6)), ERR_INVALID, r"n_q_heads \(6\)"), (lambda: select(s=step(total_new=3)), ERR_INVALID, "multiple of batch"),
-    (lambda: select(s=step(n_q_heads=65536)), ERR_UNSUPPORTED, "65535"), (lambda: select(s=step(total_new=1 << 22, max_new=1 << 22)), ERR_UNSUPPORTED, "2\\^24"),
+    (lambda: select(s=step(n_q_heads=65536)), ERR_UNSUPPORTED, "65535"), (lambda: select(s=step(total_new=1 << 20, max_new=1 << 20)), ERR_UNSUPPORTED, "2\\^22"),
     (lambda: select(s=step(total_new=-2)), ERR_INVALID, "negative"), (lambda: select(s=step(max_new=-1)), ERR_INVALID, "negative"),
     (lambda: sparse(q=N), ERR_INVALID, "q and out"), (lambda: sparse(out=N), ERR_INVALID, "q and out"), (lambda: sparse(idx=N), ERR_INVALID, "idx and count"),
     (lambda: sparse(count=N), ERR_INVALID, "idx and count"), (lambda: sparse(out=At(8)), ERR_UNSUPPORTED, "16-byte"),
@@ -133,9 +133,9 @@ def test_workspace_bytes_depend_on_no_device_data():
 def test_the_largest_descriptors():
     """At the limits, products of descriptors stay in their types (the sanitized library runs this too)."""
     for p in (pages(batch=(1 << 24) - 1, n_kv_heads=1, max_pages=(1 << 26) - 1), pages(n_kv_heads=65535, batch=255, page_rows=1024, max_pages=(1 << 20) - 1)):
-        s = step(total_new=p.batch, n_q_heads=p.n_kv_heads)
-        assert D.paged_select_workspace_bytes(p, blocks(n_select=4096), s) > 0
-        assert D.paged_sparse_attention_workspace_bytes(p, blocks(n_select=4096), step(total_new=64, max_new=64, cu_new=A, n_q_heads=p.n_kv_heads)) > 0
+        s = step(total_new=63, max_new=63, cu_new=A, n_q_heads=p.n_kv_heads)
+        assert D.paged_select_workspace_bytes(p, blocks(n_select=4096), s) >= 63 * p.n_kv_heads * 4 * (p.max_pages * p.page_rows // 16)
+        assert D.paged_sparse_attention_workspace_bytes(p, blocks(n_select=4096), s) > 0
 
 
 # --- the definition ---------------------------------------------------------------------------------------------------------
