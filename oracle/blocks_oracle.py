@@ -7,7 +7,15 @@ from __future__ import annotations
 
 import numpy as np
 
-from .paged_oracle import place, value
+from .dapq_oracle import bf16_bits_to_f64
+from .paged_oracle import code_values, place
+
+
+def rows_of(pool, name, layer, head, where):
+    """Rows of the pool, float64 [n][128], at (page, slot) each."""
+    pages, slots = (np.array(x, dtype=np.int64) for x in zip(*where))
+    row = pool[name][layer, pages, head, slots]
+    return code_values(row, pool[name + "_scales"][layer, pages, head, slots]) if name + "_scales" in pool else bf16_bits_to_f64(row)
 
 
 def unit(largest):
@@ -40,7 +48,7 @@ def bounds(pool, table, block_rows, first, lengths, max_rows, old, old_scales):
                 continue
             for layer in range(layers):
                 for head in range(heads):
-                    keys = np.stack([value(pool, "k", layer, head, (where[0], where[1] + i)) for i in range(block_rows)])
+                    keys = rows_of(pool, "k", layer, head, [(where[0], where[1] + i) for i in range(block_rows)])
                     at = (layer, where[0], head, where[1] // block_rows)
                     out[at][0], out[at][1], scales[at] = block_bounds(keys)
     return out, scales
@@ -103,7 +111,7 @@ def sparse_attention(pool, table, lengths, cu_new, max_new, q, idx, count, block
                     where = [w for w in where if w is not None]
                     if not where:
                         continue
-                    k, v = (np.stack([value(pool, name, layer, head, w) for w in where]) for name in ("k", "v"))
+                    k, v = (rows_of(pool, name, layer, head, where) for name in ("k", "v"))
                     for h in range(head * group, (head + 1) * group):
                         with np.errstate(invalid="ignore"):
                             x = k @ q[layer, r, h] * scale

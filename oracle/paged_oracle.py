@@ -62,10 +62,10 @@ def e4m3_quantise(x):
     for candidate in range(-116, 120):
         e = np.where(largest > 464.0 * 2.0 ** (candidate - 1), candidate, e)
     y = np.abs(g0) / (2.0 ** e)[..., None]
-    distance = np.abs(y[..., None] - E4M3_LEVELS)
-    nearest = distance == distance.min(-1, keepdims=True)
-    prefer = 1 - np.arange(127) % 2                             # of two nearest levels the even code
-    code = np.argmax(nearest * (1 + prefer), -1) + np.where(np.signbit(g0), 128, 0)
+    above = np.clip(np.searchsorted(E4M3_LEVELS, y), 1, 126)
+    to_low, to_high = y - E4M3_LEVELS[above - 1], E4M3_LEVELS[above] - y
+    code = np.where((to_high < to_low) | ((to_high == to_low) & (above % 2 == 0)), above, above - 1)  # of two nearest levels the even code
+    code = code + np.where(np.signbit(g0), 128, 0)
     return np.where(bad[..., None], 0, code).reshape(x.shape).astype(np.uint8), np.where(bad, 255, e + 127).astype(np.uint8)
 
 

@@ -264,8 +264,8 @@ struct PagedReadParams {
   int32_t batch, max_rows;
 };
 
-// 16 lanes to a row, two rows of K and of V to a lane group.
-template <int FMT, bool STREAM>
+// 16 lanes to a row, two rows of K and of V to a lane group.  STREAM_IN: hints of the loads of bf16 rows and E4M3 codes (FP4 codes have none), STREAM: of the stores.
+template <int FMT, bool STREAM_IN, bool STREAM>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadParams p) {
   touch_args<sizeof(PagedReadParams)>();
   constexpr int ROWS = 2;
@@ -288,12 +288,12 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadParams p) {
       x[r][0][0] = *reinterpret_cast<const unsigned*>(p.pool.k + row[r] * kCodeBytes<kFp4> + ch * 4);
       x[r][1][0] = *reinterpret_cast<const unsigned*>(p.pool.v + row[r] * kCodeBytes<kFp4> + ch * 4);
     } else if constexpr (FMT == kE4m3) {
-      const u32x2 k = get<STREAM>(reinterpret_cast<const u32x2*>(p.pool.k + row[r] * kCodeBytes<kE4m3> + ch * 8));
-      const u32x2 v = get<STREAM>(reinterpret_cast<const u32x2*>(p.pool.v + row[r] * kCodeBytes<kE4m3> + ch * 8));
+      const u32x2 k = get<STREAM_IN>(reinterpret_cast<const u32x2*>(p.pool.k + row[r] * kCodeBytes<kE4m3> + ch * 8));
+      const u32x2 v = get<STREAM_IN>(reinterpret_cast<const u32x2*>(p.pool.v + row[r] * kCodeBytes<kE4m3> + ch * 8));
       x[r][0][0] = k[0], x[r][0][1] = k[1], x[r][1][0] = v[0], x[r][1][1] = v[1];
     } else {
-      x[r][0] = get<STREAM>(reinterpret_cast<const u32x4*>(p.pool.k + row[r] * kRowBytes + ch * 16));
-      x[r][1] = get<STREAM>(reinterpret_cast<const u32x4*>(p.pool.v + row[r] * kRowBytes + ch * 16));
+      x[r][0] = get<STREAM_IN>(reinterpret_cast<const u32x4*>(p.pool.k + row[r] * kRowBytes + ch * 16));
+      x[r][1] = get<STREAM_IN>(reinterpret_cast<const u32x4*>(p.pool.v + row[r] * kRowBytes + ch * 16));
     }
     if constexpr (FMT != kBf16) {
       scale[r][0] = p.pool.k_scales[row[r] * 4 + (ch >> 2)];
@@ -319,7 +319,10 @@ auto gather_of(int64_t moved) {
 }
 template <int FMT>
 auto read_of(int64_t moved) {
-  return moved >= kStreamRead ? paged_read_kernel<FMT, true> : paged_read_kernel<FMT, false>;
+  // E4M3 codes that an append has just written are in the caches, up to the size of kStreamIn: 64 sequences of 16..97 rows (22 MB) 9.8 -> 7.4 us without hints
+  // of the loads, 814 MB 154 -> 152 with them.
+  if (FMT == kE4m3 && moved < kStreamIn) return moved >= kStreamRead ? paged_read_kernel<FMT, false, true> : paged_read_kernel<FMT, false, false>;
+  return moved >= kStreamRead ? paged_read_kernel<FMT, true, true> : paged_read_kernel<FMT, false, false>;
 }
 
 }  // namespace

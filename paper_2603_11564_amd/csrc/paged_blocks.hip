@@ -292,12 +292,10 @@ constexpr int kColTiles = 8, kColTileBytes = 4096;  // column tiles in LDS, at m
 // COLUMNS: kOne: one column tile in all, whose operand stays in registers; kMany; kWide: a token has more than 16 query heads, and several column tiles.
 // REGS: of the Choice of the same workgroup, which has all tiles of the sequence and keeps their keys in LDS; 0: the keys go to the workspace.
 enum Columns { kOne, kMany, kWide };
-constexpr int kScoreWaves = 4, kWholeWaves = 8;
-template <int COLUMNS, int REGS>
-__global__ __launch_bounds__(64 * (REGS > 0 ? kWholeWaves : kScoreWaves)) void paged_scores_kernel(SelectParams p) {
+template <int COLUMNS, int WAVES, int REGS>
+__global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p) {
   touch_args<sizeof(SelectParams)>();
   constexpr bool WIDE = COLUMNS == kWide, WHOLE = REGS > 0;
-  constexpr int WAVES = WHOLE ? kWholeWaves : kScoreWaves;
   extern __shared__ char lds[];  // column tiles; the units of their columns; WHOLE: keys
   float* units = reinterpret_cast<float*>(lds + p.col_tiles * kColTileBytes);
   unsigned* whole_keys = reinterpret_cast<unsigned*>(units + 16 * p.col_tiles);
@@ -565,7 +563,6 @@ __global__ __launch_bounds__(256) void paged_choose_long_kernel(SelectParams p) 
   if (tid == 0) p.count[blockIdx.x] = (int)(above + (equal < cut.equal ? equal : cut.equal));
 }
 
-constexpr int kWholeKeys = 64 << 10;  // bytes of keys in LDS, at most
 struct SelectPlan {
   int64_t stride, chunk, chunks, columns;  // columns: workgroups along the column tiles
   int cols_log2, col_tiles;
@@ -586,8 +583,12 @@ SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
   plan.columns = plan.columns < 1 ? 1 : (plan.columns > 65535 ? 65535 : plan.columns);
   const int64_t items = (int64_t)pages->n_layers * pages->batch * pages->n_kv_heads;
   plan.lds = plan.col_tiles * (kColTileBytes + 64);
+  // One kernel, a workgroup for all blocks of an item, or a kernel for chunks of them and one for the choice.  A workgroup takes 0.11 us a tile of its own, where the bytes
+  // of all take 0.75 ns (half of the table in use), and a second kernel some 3 us; tokens are chosen for one after the other.  Us, one kernel / two, 4 query heads of 8 KV
+  // heads, sequences x blocks: 1 x 128 6.5 / 8.9, 1 x 512 8.9 / 9.1, 1 x 2048 20.0 / 9.4, 8 x 512 9.1 / 9.8, 16 x 2048 20.9 / 21.4, 16 x 256..8192 65 / 42, 32 x 1024 16.0 / 20.5, 64 x
+  // 512 16.6 / 20.9, 64 x 2048 53 / 64; two tokens of 64 x 256 15.0 / 16.2, four of 16 x 512 17.1 / 12.2.
   const int64_t key_bytes = most * plan.stride * 4;
-  plan.whole = plan.cols_log2 <= 4 && plan.columns == 1 && key_bytes <= kWholeKeys && plan.stride <= 8192 && items >= 128;
+  plan.whole = plan.cols_log2 <= 4 && plan.col_tiles == 1 && most <= 2 && plan.stride <= 8192 && 0.11 * (double)tiles < 3.0 + 0.5 * 0.75e-3 * (double)(tiles * items);
   if (plan.whole) {
     plan.lds += (int)key_bytes;
     plan.chunk = tiles;
@@ -689,16 +690,16 @@ extern "C" DAPQ_API int dapq_paged_select(const dapq_pages* pages, const dapq_bl
   const hipStream_t on = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)((int64_t)p.items * p.batch * p.chunks), (unsigned)plan.columns);
   if (plan.whole) {
-    auto kernel = plan.col_tiles == 1 ? (plan.stride <= 2048 ? paged_scores_kernel<kOne, 1> : paged_scores_kernel<kOne, 4>)
-                                      : (plan.stride <= 2048 ? paged_scores_kernel<kMany, 1> : paged_scores_kernel<kMany, 4>);
-    rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), kColTiles * (kColTileBytes + 64) + kWholeKeys);
+    const int waves = plan.stride <= 256 ? 4 : 8;
+    auto kernel = plan.stride <= 256 ? paged_scores_kernel<kOne, 4, 1> : (plan.stride <= 2048 ? paged_scores_kernel<kOne, 8, 1> : paged_scores_kernel<kOne, 8, 4>);
+    rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), kColTileBytes + 64 + 2 * 8192 * 4);
     if (rc != DAPQ_OK) return rc;
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * kWholeWaves), plan.lds, on, p);
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), plan.lds, on, p);
     DAPQ_HIP_LAUNCH_CHECK("paged_scores_kernel");
     return DAPQ_OK;
   }
-  hipLaunchKernelGGL((plan.cols_log2 > 4 ? paged_scores_kernel<kWide, 0> : (plan.col_tiles == 1 ? paged_scores_kernel<kOne, 0> : paged_scores_kernel<kMany, 0>)),
-                     grid, dim3(64 * kScoreWaves), plan.lds, on, p);
+  hipLaunchKernelGGL((plan.cols_log2 > 4 ? paged_scores_kernel<kWide, 4, 0> : (plan.col_tiles == 1 ? paged_scores_kernel<kOne, 4, 0> : paged_scores_kernel<kMany, 4, 0>)),
+                     grid, dim3(256), plan.lds, on, p);
   DAPQ_HIP_LAUNCH_CHECK("paged_scores_kernel");
   const unsigned rows = (unsigned)((int64_t)p.items * p.total_new);
   if (plan.stride <= 1024) hipLaunchKernelGGL((paged_choose_kernel<4, 1>), dim3(rows), dim3(256), 0, on, p);

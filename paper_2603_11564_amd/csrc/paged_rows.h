@@ -13,6 +13,7 @@ struct SparseParams : PagedAttentionParams {
   const int32_t *idx, *count;
   int32_t block_shift, n_select;
   int32_t parts_each;  // workgroups of an item
+  int32_t most_tiles;  // of n_select blocks
 };
 template <bool SPARSE>
 using RowParams = std::conditional_t<SPARSE, SparseParams, PagedAttentionParams>;
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
     entry1 = p.pool.table[table + (row_of1 < 0 ? 0 : row_of1 >> p.pool.page_shift)];
   };
   // this workgroup's item, and its part of it
-  int seq, item, part = 0, parts = 1;
+  int seq, item, part = 0, parts = 1, tile0, tile1;
   Sequence s;
   int seen_of_token = 0, chosen_count = 0;  // SPARSE
   if constexpr (SPARSE) {
@@ -155,15 +156,21 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
     part = blockIdx.y;
     parts = p.parts_each;
     const int kept = p.count[blockIdx.x];
+    // parts are cut from the most rows that there may be, so that the first blocks are on their way before the count is known
+    tile0 = uniform(p.most_tiles * part / parts);
+    tile1 = uniform(p.most_tiles * (part + 1) / parts);
+    blocks_of((tile0 + wave + (int64_t)kRowWaves * lane) * kTile);
     int t;
     if (!find_token(p.cu_new, p.batch, p.each_new, p.max_new, r, lane, &seq, &t)) return;
     seq = uniform(seq);
+    entries_of_blocks((int64_t)seq * p.pool.max_pages);
     const int before = uniform(p.lengths[seq]);
     const int64_t most = (int64_t)p.pool.max_pages << p.pool.page_shift, n = (int64_t)before + t + 1;
     seen_of_token = uniform((int)(n < 0 ? 0 : (n < most ? n : most)));
     chosen_count = uniform(kept < 0 ? 0 : (kept < p.n_select ? kept : p.n_select));
     const int64_t rows = (int64_t)chosen_count << p.block_shift;
     s = {r, 1, before, (int)((rows + kTile - 1) / kTile)};
+    tile1 = tile1 < s.tiles ? tile1 : s.tiles;
   } else if constexpr (SPLIT) {
     Tiles t = tiles_of_64(p, 0, lane);
     int64_t total = from_lane(t.upto, 63);
@@ -196,8 +203,10 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
     s = uniform_sequence(p, seq);
     if (s.tiles == 0) return;
   }
-  const int tile0 = SPLIT ? uniform((int)((int64_t)s.tiles * part / parts)) : 0;
-  const int tile1 = SPLIT ? uniform((int)((int64_t)s.tiles * (part + 1) / parts)) : s.tiles;
+  if constexpr (!SPARSE) {
+    tile0 = SPLIT ? uniform((int)((int64_t)s.tiles * part / parts)) : 0;
+    tile1 = SPLIT ? uniform((int)((int64_t)s.tiles * (part + 1) / parts)) : s.tiles;
+  }
 
   {
     const int layer = item / p.pool.n_kv_heads, head = item - layer * p.pool.n_kv_heads;
@@ -235,10 +244,12 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
     auto load_pages = [&](int k) {
       const int64_t row = ((int64_t)tile0 + wave + (int64_t)kRowWaves * (k + opaque(lane))) * kTile;
       if constexpr (SPARSE) {
-        blocks_of(row);
+        if (k > 0) {
+          blocks_of(row);
+          entries_of_blocks((int64_t)seq * p.pool.max_pages);
+        }
         if (row >= chosen_rows) row_of0 = -1;
         if (row + 16 >= chosen_rows) row_of1 = -1;
-        entries_of_blocks((int64_t)seq * p.pool.max_pages);
       } else if (SPLIT || k > 0) {
         entries_of((int64_t)seq * p.pool.max_pages, row, &entry0, &entry1);
       }
@@ -575,8 +586,9 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
 
 // The items that several workgroups share.  WAVES: a column has all waves of a workgroup, which take its parts in turn and meet in LDS (few items, many
 // parts), or one (32 sequences, 32 columns, 2 parts each: the whole call 150 -> 138 us).
+// EARLY: parts whose sums are asked for before their weights are known.
 constexpr int kJoinWaves = 8, kJoinEarly = 4;
-template <int COLS, int WAVES, bool SPARSE>
+template <int COLS, int WAVES, bool SPARSE, int EARLY = kJoinEarly>
 __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(RowParams<SPARSE> p) {
   __shared__ float wave_sums[kJoinWaves][kHeadDim + 2];
   const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : uniform(threadIdx.x >> 6);
@@ -618,9 +630,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(RowParams<S
     const int mine = i0 + WAVES * lane, n = (parts - i0 + WAVES - 1) / WAVES < 64 ? (parts - i0 + WAVES - 1) / WAVES : 64;
     const float r = mine < parts ? part(mine)[COLS * kHeadDim + col] : -INFINITY;
     float w = mine < parts ? part(mine)[COLS * (kHeadDim + 1) + col] : 0.0f;
-    f32x2 early[kJoinEarly];  // (their loads need no weights)
+    f32x2 early[EARLY];  // (their loads need no weights)
 #pragma unroll
-    for (int i = 0; i < kJoinEarly; ++i) early[i] = *reinterpret_cast<const f32x2*>(part(i0 + WAVES * (i < n ? i : n - 1)) + col * kHeadDim + 2 * lane);
+    for (int i = 0; i < EARLY; ++i) early[i] = *reinterpret_cast<const f32x2*>(part(i0 + WAVES * (i < n ? i : n - 1)) + col * kHeadDim + 2 * lane);
     float top = r;
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     const float moved = fmaxf(m, top);
@@ -638,10 +650,10 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(RowParams<S
       o[1] = fmaf(fi, x[1], o[1]);
     };
 #pragma unroll
-    for (int i = 0; i < kJoinEarly; ++i)
+    for (int i = 0; i < EARLY; ++i)
       if (i < n) add(i, early[i]);
 #pragma unroll 4
-    for (int i = kJoinEarly; i < n; ++i) add(i, *reinterpret_cast<const f32x2*>(part(i0 + WAVES * i) + col * kHeadDim + 2 * lane));
+    for (int i = EARLY; i < n; ++i) add(i, *reinterpret_cast<const f32x2*>(part(i0 + WAVES * i) + col * kHeadDim + 2 * lane));
   }
   if constexpr (WAVES > 1) {
     *reinterpret_cast<f32x2*>(&wave_sums[wave][2 * lane]) = o;

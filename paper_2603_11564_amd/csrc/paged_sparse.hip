@@ -10,7 +10,7 @@ namespace {
 struct SparsePlan {
   int cols, chunks;  // columns of the kernel, and how many such runs of a token's query heads there are
   int64_t items;
-  int parts;
+  int parts, tiles;
 };
 SparsePlan sparse_plan(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step) {
   SparsePlan plan;
@@ -20,6 +20,7 @@ SparsePlan sparse_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
   plan.items = (int64_t)pages->n_layers * step->total_new * pages->n_kv_heads;
   const int64_t all = most_blocks(pages, blocks), rows = (blocks->n_select < all ? blocks->n_select : all) * blocks->block_rows;
   const int64_t tiles = (rows + kTile - 1) / kTile;
+  plan.tiles = (int)(((int64_t)blocks->n_select * blocks->block_rows + kTile - 1) / kTile);  // (up to 2^17: parts_each times it stays below 2^31)
   const int64_t resident = plan.cols == 32 ? 512 : 768, items = plan.items * plan.chunks;
   int64_t parts = items > 0 ? resident / items : 1;
   if (parts > tiles / kRowWaves) parts = tiles / kRowWaves;
@@ -39,8 +40,8 @@ int launch_sparse(const SparseParams& p, const SparsePlan& plan, hipStream_t str
   DAPQ_HIP_LAUNCH_CHECK("paged_rows_kernel");
   if (SPLIT) {
     const unsigned cols = (unsigned)(p.group < kCols ? p.group : kCols);
-    if (plan.items < 128) hipLaunchKernelGGL((paged_join_kernel<kCols, kJoinWaves, true>), dim3((unsigned)plan.items, cols, (unsigned)plan.chunks), dim3(64 * kJoinWaves), 0, stream, p);
-    else hipLaunchKernelGGL((paged_join_kernel<kCols, 1, true>), dim3((unsigned)plan.items, (cols + kJoinWaves - 1) / kJoinWaves, (unsigned)plan.chunks), dim3(64 * kJoinWaves), 0, stream, p);
+    if (plan.items < 128 && plan.parts > 16) hipLaunchKernelGGL((paged_join_kernel<kCols, kJoinWaves, true>), dim3((unsigned)plan.items, cols, (unsigned)plan.chunks), dim3(64 * kJoinWaves), 0, stream, p);
+    else hipLaunchKernelGGL((paged_join_kernel<kCols, 1, true, 16>), dim3((unsigned)plan.items, (cols + kJoinWaves - 1) / kJoinWaves, (unsigned)plan.chunks), dim3(64 * kJoinWaves), 0, stream, p);
     DAPQ_HIP_LAUNCH_CHECK("paged_join_kernel");
   }
   return DAPQ_OK;
@@ -92,6 +93,7 @@ extern "C" DAPQ_API int dapq_paged_sparse_attention(const dapq_pages* pages, con
   p.n_select = blocks->n_select;
   const SparsePlan plan = sparse_plan(pages, blocks, step);
   p.parts_each = plan.parts;
+  p.most_tiles = plan.tiles;
   const hipStream_t on = static_cast<hipStream_t>(stream);
   return pages->format == DAPQ_PAGES_BF16 ? launch_sparse<kBf16>(p, plan, on) : (pages->format == DAPQ_PAGES_FP4 ? launch_sparse<kFp4>(p, plan, on) : launch_sparse<kE4m3>(p, plan, on));
 }

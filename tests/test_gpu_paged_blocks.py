@@ -332,17 +332,16 @@ SPARSE = [  # layers, kv heads, group, page_rows, block_rows, lengths, new, n_se
     (1, 2, 70, 16, 16, [90, 30], [1, 2], 4),
     (1, 2, 4, 16, 16, [33, 0, 250], [4, 4, 4], 9),
     (2, 1, 3, 16, 16, [0, 5, 40], [37, 0, 20], 2),
-    (1, 2, 2, 16, 16, [3 * b for b in range(70)], [b % 3 for b in range(70)], 4),
+    (1, 2, 2, 16, 16, [b for b in range(70)], [b % 3 for b in range(70)], 4),
     (1, 1, 4, 1024, 512, [3000], [1], 3),
     (1, 2, 4, 64, 16, [4000], [1], 200),
-    (1, 8, 4, 16, 16, [300] * 40, [1] * 40, 3),
+    (1, 8, 4, 16, 16, [70] * 40, [1] * 40, 3),
 ]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("softcap", [0.0, 20.0, 100.0])
-@pytest.mark.parametrize("case", range(len(SPARSE)))
-def test_sparse_attention(fmt, softcap, case):
+@pytest.mark.parametrize("case,softcap", [(i, 0.0) for i in range(len(SPARSE))] + [(i, c) for i in (1, 3, 4, 5, 7, 12) for c in (20.0, 100.0)])
+def test_sparse_attention(fmt, case, softcap):
     layers, heads, group, page_rows, block_rows, lengths, new, n_select = SPARSE[case]
     rng = np.random.default_rng(700 + case)
     rows = [h + n for h, n in zip(lengths, new)]
