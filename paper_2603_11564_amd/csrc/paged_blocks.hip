@@ -125,14 +125,14 @@ __device__ __forceinline__ int blocks_seen(const SelectParams& p, int before, in
   return ((n < 0 ? 0 : (n < most ? n : most)) + (1 << p.block_shift) - 1) >> p.block_shift;
 }
 
-// Four values, each the largest of the 2^log2 lanes that a lane stands among (up to 16).  Lanes that agree already are taken by mirrors of 8 and 16 lanes.
+// Four keys, each the largest of the 2^log2 lanes that a lane stands among (up to 16).  Lanes that agree already are taken by mirrors of 8 and 16 lanes.
 constexpr int kMirror8 = 0x141, kMirror16 = 0x140;
 template <int CTRL>
-__device__ __forceinline__ void with_lanes(float (&x)[4]) {
+__device__ __forceinline__ void with_lanes(u32x4& x) {
 #pragma unroll
-  for (int v = 0; v < 4; ++v) x[v] = fmaxf(x[v], __uint_as_float(dpp<CTRL>(__float_as_uint(x[v]))));
+  for (int v = 0; v < 4; ++v) x[v] = larger(x[v], dpp<CTRL>(x[v]));
 }
-__device__ __forceinline__ void largest_of_lanes(float (&x)[4], int log2) {
+__device__ __forceinline__ void largest_of_lanes(u32x4& x, int log2) {
   if (log2 == 0) return;
   with_lanes<kXor1>(x);
   if (log2 == 1) return;
@@ -284,7 +284,8 @@ struct Choice {
   }
 };
 
-constexpr int kColTiles = 8, kColTileBytes = 4096;  // column tiles in LDS, at most; u+ and u- of 16 columns
+constexpr int kAhead = 1;
+constexpr int kColTiles = 8, kColTileBytes = 4096;  // column tiles in LDS, at most; u+ and u- of 16 columns, and as much is a tile of bounds
 
 // The score is a product of whole numbers of 8 bits, 256 long: with u+ = max(u, 0) and u- = min(u, 0), max(u * upper, u * lower) = u+ * upper + u- * lower.
 // D[block][column] = bounds (A, 16 blocks) x (u+, u-) (B, 16 columns: query heads of a token, padded to a power of two) on v_mfma_i32_16x16x64_i8, exact.
@@ -296,11 +297,12 @@ template <int COLUMNS, int WAVES, int REGS>
 __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p) {
   touch_args<sizeof(SelectParams)>();
   constexpr bool WIDE = COLUMNS == kWide, WHOLE = REGS > 0;
-  extern __shared__ char lds[];  // column tiles; the units of their columns; WHOLE: keys
-  float* units = reinterpret_cast<float*>(lds + p.col_tiles * kColTileBytes);
+  extern __shared__ char lds[];  // column tiles; a tile of bounds to a wave; the units of the columns; WHOLE: keys
+  float* units = reinterpret_cast<float*>(lds + (p.col_tiles + WAVES) * kColTileBytes);
   unsigned* whole_keys = reinterpret_cast<unsigned*>(units + 16 * p.col_tiles);
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kg = lane >> 4;
   const int wave = uniform(tid >> 6);
+  char* turned = lds + (p.col_tiles + wave) * kColTileBytes;
   // (chunks of the same number follow each other: workgroups go round the chip's eight parts, and late chunks are those that sequences do not have)
   const int all_items = p.items * p.batch, chunk = blockIdx.x / all_items, of_item = blockIdx.x - chunk * all_items;
   const int seq = uniform_quotient(of_item, p.items, p.inv_items), item = of_item - seq * p.items;
@@ -312,7 +314,9 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
     const int e = (16 * k + n) >> to_page;
     return table[e < p.pool.max_pages ? e : p.pool.max_pages - 1];
   };
-  int page = page_of(chunk * p.chunk + wave);
+  int pages[kAhead + 1];
+#pragma unroll
+  for (int i = 0; i <= kAhead; ++i) pages[i] = page_of(chunk * p.chunk + wave + i * WAVES);
   const int first = uniform(p.cu_new == nullptr ? seq * p.each_new : p.cu_new[seq]);
   int tokens = p.cu_new == nullptr ? p.each_new : uniform(p.cu_new[seq + 1]) - first;
   tokens = tokens < p.max_new ? tokens : p.max_new;
@@ -320,7 +324,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
   const int before = uniform(p.lengths[seq]);
   const int tiles = (blocks_seen(p, before, tokens - 1) + 15) >> 4, tile0 = chunk * p.chunk, tile1 = tile0 + p.chunk < tiles ? tile0 + p.chunk : tiles;
   if (!WHOLE && tile0 >= tile1) return;
-  // A tile is asked for while the one before it is used, its pages one tile earlier.
+  // A tile is asked for kAhead tiles before it is used, its pages one tile earlier.
   struct Tile {
     i32x4 a[4];
     int scale;  // -1 on no page
@@ -329,10 +333,13 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
   auto fetch = [&](Tile& tile, int k, int page) {
     const int block = 16 * k + n;
     const bool there = k < tile1 && page >= 0 && page < p.pool.n_pages && block >> to_page < p.pool.max_pages;
-    const int64_t at = there ? head_of_layer + (((int64_t)page * p.pool.n_kv_heads) << to_page) + (block & ((1 << to_page) - 1)) : 0;
-    const uint8_t* src = p.bounds + at * (2 * kHeadDim) + 16 * kg;
+    // (blocks of a pool are below 2^32)
+    const unsigned at = there ? (unsigned)(head_of_layer + (((int64_t)page * p.pool.n_kv_heads) << to_page) + (block & ((1 << to_page) - 1))) : 0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) tile.a[i] = *reinterpret_cast<const i32x4*>(src + 64 * i);
+    for (int i = 0; i < 4; ++i) {
+      const unsigned of_lane = (unsigned)__shfl((int)at, 4 * i + kg, 64);
+      tile.a[i] = *reinterpret_cast<const i32x4*>(p.bounds + (uint64_t)of_lane * (2 * kHeadDim) + ((n ^ (4 * i + kg)) << 4));
+    }
     const int scale = p.scales[at];
     tile.scale = there ? scale : -1;
   };
@@ -342,8 +349,10 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
   for (int64_t t0 = WIDE ? blockIdx.y : 0; t0 < (WIDE ? tokens : 1); t0 += gridDim.y) {
     for (int c0 = WIDE ? 0 : blockIdx.y * p.col_tiles; c0 < all; c0 += WIDE ? p.col_tiles : (int)gridDim.y * p.col_tiles) {
       const int here = COLUMNS == kOne ? 1 : (all - c0 < p.col_tiles ? all - c0 : p.col_tiles);
-      Tile even, odd;
-      if (t0 > blockIdx.y || c0 > 0) page = page_of(tile0 + wave);
+      Tile ring[kAhead + 1];
+      if (t0 > blockIdx.y || c0 > 0)
+#pragma unroll
+        for (int i = 0; i <= kAhead; ++i) pages[i] = page_of(tile0 + wave + i * WAVES);
       // 16 lanes to a column, eight channels to a lane; columns that there are not are the last one that there is
       const int col = tid >> 4 & 15, o = tid & 15;
       auto query = [&](int c) {
@@ -354,8 +363,9 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
         return *reinterpret_cast<const u32x4*>(p.q + layer * p.q_stride_layer + (int64_t)(first + token) * p.q_stride_row + (int64_t)h * p.q_stride_head + 8 * o);
       };
       u32x4 x = query(tid >> 8);
-      fetch(even, tile0 + wave, page);
-      page = page_of(tile0 + wave + WAVES);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) fetch(ring[i], tile0 + wave + i * WAVES, pages[i]);
+      int page = pages[kAhead];
       for (int c = tid >> 8; c < here; c += WAVES / 4) {
         if (c >= WAVES / 4) x = query(c);
         unsigned largest = larger(larger(larger_magnitude(x[0]), larger_magnitude(x[1])), larger(larger_magnitude(x[2]), larger_magnitude(x[3])));
@@ -395,17 +405,20 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
       unsigned* const to0 = (WHOLE ? whole_keys + token0 * p.stride : p.keys + (((int64_t)layer * p.total_new + first + token0) * p.pool.n_kv_heads + head) * p.stride) + 4 * kg;
       const bool writes = (n & ((1 << log2) - 1)) == 0;
       auto use = [&](const Tile& tile, int k) {
+        // 16 lanes have brought in a block, whole lines of it; as operand a lane has its own: through LDS, with the 16 bytes of a block permuted by its number
+        i32x4 a[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<i32x4*>(turned + 1024 * i + 16 * lane) = tile.a[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const i32x4*>(turned + 256 * n + (((4 * i + kg) ^ n) << 4));
         const bool plain = 16 * k >= middle0 && 16 * k + 16 <= middle1 && !__any(tile.scale < 0 || tile.scale == 255);
         float factor[4];  // of this lane's blocks
         const float mine = power_of_two(tile.scale < 0 ? 0 : tile.scale);
 #pragma unroll
         for (int v = 0; v < 4; ++v) factor[v] = __shfl(mine, 4 * kg + v, 64);
-        auto put = [&](float (&best)[4], int c) {
+        auto put = [&](u32x4 keys, int c) {
           const int token = WIDE ? token0 : token0 + c * each;
-          u32x4 keys;
-          largest_of_lanes(best, log2);
-#pragma unroll
-          for (int v = 0; v < 4; ++v) keys[v] = key_of(best[v] * factor[v]);
+          largest_of_lanes(keys, log2);
           if (!plain) {
             const int seen = blocks_seen(p, before, token);
 #pragma unroll
@@ -426,33 +439,34 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
             *to = keys;
           }
         };
-        float of_token[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        u32x4 of_token = {0, 0, 0, 0};
 #pragma unroll 2
         for (int c = 0; c < here; ++c) {
           i32x4 up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            up = __builtin_amdgcn_mfma_i32_16x16x64_i8(tile.a[i], COLUMNS == kOne ? own[i] : operand(c, i), up, 0, 0, 0);
-            down = __builtin_amdgcn_mfma_i32_16x16x64_i8(tile.a[2 + i], COLUMNS == kOne ? own[2 + i] : operand(c, 2 + i), down, 0, 0, 0);
+            up = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], COLUMNS == kOne ? own[i] : operand(c, i), up, 0, 0, 0);
+            down = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[2 + i], COLUMNS == kOne ? own[2 + i] : operand(c, 2 + i), down, 0, 0, 0);
           }
           const float unit = COLUMNS == kOne ? own_unit : units[c * 16 + n];
-          float best[4];
+          u32x4 keys;
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            best[v] = (float)(up[v] + down[v]) * unit;
-            of_token[v] = fmaxf(of_token[v], best[v]);
+            keys[v] = key_of((float)(up[v] + down[v]) * unit * factor[v]);
+            of_token[v] = larger(of_token[v], keys[v]);
           }
-          if (!WIDE) put(best, c);
+          if (!WIDE) put(keys, c);
         }
         if (WIDE) put(of_token, 0);
       };
-      for (int k = tile0 + wave; k < tile1; k += 2 * WAVES) {
-        fetch(odd, k + WAVES, page);
-        page = page_of(k + 2 * WAVES);
-        use(even, k);
-        fetch(even, k + 2 * WAVES, page);
-        page = page_of(k + 3 * WAVES);
-        if (k + WAVES < tile1) use(odd, k + WAVES);
+      for (int k0 = tile0 + wave; k0 < tile1; k0 += (kAhead + 1) * WAVES) {
+#pragma unroll
+        for (int i = 0; i <= kAhead; ++i) {
+          const int k = k0 + i * WAVES;
+          fetch(ring[(i + kAhead) % (kAhead + 1)], k + kAhead * WAVES, page);
+          page = page_of(k + (kAhead + 1) * WAVES);
+          if (k < tile1) use(ring[i], k);
+        }
       }
       if (WHOLE || COLUMNS != kOne) __syncthreads();
     }
@@ -567,7 +581,7 @@ struct SelectPlan {
   int64_t stride, chunk, chunks, columns;  // columns: workgroups along the column tiles
   int cols_log2, col_tiles;
   bool whole;  // a workgroup scores all blocks of a sequence and KV head and chooses them
-  int lds;
+  int waves, lds;
 };
 SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step) {
   SelectPlan plan;
@@ -588,12 +602,14 @@ SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
   // heads, sequences x blocks: 1 x 128 6.5 / 8.9, 1 x 512 8.9 / 9.1, 1 x 2048 20.0 / 9.4, 8 x 512 9.1 / 9.8, 16 x 2048 20.9 / 21.4, 16 x 256..8192 65 / 42, 32 x 1024 16.0 / 20.5, 64 x
   // 512 16.6 / 20.9, 64 x 2048 53 / 64; two tokens of 64 x 256 15.0 / 16.2, four of 16 x 512 17.1 / 12.2.
   const int64_t key_bytes = most * plan.stride * 4;
-  plan.whole = plan.cols_log2 <= 4 && plan.col_tiles == 1 && most <= 2 && plan.stride <= 8192 && 0.11 * (double)tiles < 3.0 + 0.5 * 0.75e-3 * (double)(tiles * items);
+  plan.whole = plan.cols_log2 <= 4 && plan.col_tiles == 1 && most <= 2 && plan.stride <= 8192 && items < 1 << 20 && 0.11 * (double)tiles < 3.0 + 0.5 * 0.75e-3 * (double)(tiles * items);
+  plan.waves = plan.whole && plan.stride > 256 ? 8 : 4;
+  plan.lds += plan.waves * kColTileBytes;
   if (plan.whole) {
     plan.lds += (int)key_bytes;
     plan.chunk = tiles;
   } else {
-    plan.chunk = (tiles * items + 2047) / 2048;
+    plan.chunk = (tiles * items + 1023) / 1024;
     plan.chunk = plan.chunk < 4 ? 4 : (plan.chunk + 3) / 4 * 4;
   }
   plan.chunks = (tiles + plan.chunk - 1) / plan.chunk;
@@ -637,7 +653,8 @@ extern "C" DAPQ_API int dapq_paged_bounds(const dapq_pages* pages, const dapq_bl
   p.block_shift = __builtin_ctz((unsigned)blocks->block_rows);
   p.max_rows = max_rows;
   const int64_t all = most_blocks(pages, blocks), most = ((int64_t)max_rows + blocks->block_rows - 1) / blocks->block_rows;
-  const int64_t groups = ((most < all ? most : all) + 3) / 4;  // (below 2^24: blocks are below 2^26)
+  const int64_t groups = ((most < all ? most : all) + 3) / 4;
+  DAPQ_REQUIRE(groups * 256 < (int64_t)1 << 32, DAPQ_ERR_UNSUPPORTED, "max_rows (%d) is too large", max_rows);
   auto kernel = pages->format == DAPQ_PAGES_BF16 ? paged_bounds_kernel<kBf16> : (pages->format == DAPQ_PAGES_FP4 ? paged_bounds_kernel<kFp4> : paged_bounds_kernel<kE4m3>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)(pages->n_layers * pages->n_kv_heads), (unsigned)pages->batch), dim3(256), 0,
                      static_cast<hipStream_t>(stream), p);
@@ -690,11 +707,10 @@ extern "C" DAPQ_API int dapq_paged_select(const dapq_pages* pages, const dapq_bl
   const hipStream_t on = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)((int64_t)p.items * p.batch * p.chunks), (unsigned)plan.columns);
   if (plan.whole) {
-    const int waves = plan.stride <= 256 ? 4 : 8;
-    auto kernel = plan.stride <= 256 ? paged_scores_kernel<kOne, 4, 1> : (plan.stride <= 2048 ? paged_scores_kernel<kOne, 8, 1> : paged_scores_kernel<kOne, 8, 4>);
-    rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), kColTileBytes + 64 + 2 * 8192 * 4);
+    auto kernel = plan.waves == 4 ? paged_scores_kernel<kOne, 4, 1> : (plan.stride <= 2048 ? paged_scores_kernel<kOne, 8, 1> : paged_scores_kernel<kOne, 8, 4>);
+    rc = set_max_dynamic_lds(reinterpret_cast<const void*>(kernel), 9 * kColTileBytes + 64 + 2 * 8192 * 4);
     if (rc != DAPQ_OK) return rc;
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), plan.lds, on, p);
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * plan.waves), plan.lds, on, p);
     DAPQ_HIP_LAUNCH_CHECK("paged_scores_kernel");
     return DAPQ_OK;
   }

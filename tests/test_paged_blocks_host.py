@@ -70,6 +70,7 @@ REFUSED = [
     (lambda: select(b=blocks(bounds=N)), ERR_INVALID, "bounds and scales"), (lambda: select(b=blocks(bounds=At(8))), ERR_UNSUPPORTED, "16-byte"),
     (lambda: bounds(b=blocks(bounds=At(4))), ERR_UNSUPPORTED, "16-byte"), (lambda: bounds(lengths=N), ERR_INVALID, "lengths"),
     (lambda: bounds(rows=-1), ERR_INVALID, r"max_rows \(-1\)"), (lambda: bounds(p=pages(batch=70000)), ERR_UNSUPPORTED, "65535"),
+    (lambda: bounds(p=pages(max_pages=(1 << 26) - 1), rows=2 ** 31 - 1), ERR_UNSUPPORTED, "too large"),
     (lambda: select(q=N), ERR_INVALID, "q, idx and count"), (lambda: select(idx=N), ERR_INVALID, "q, idx and count"),
     (lambda: select(count=N), ERR_INVALID, "q, idx and count"), (lambda: select(q=At(8)), ERR_UNSUPPORTED, "q must be 16-byte"),
     (lambda: select(work=N), ERR_INVALID, "workspace is NULL"), (lambda: select(work=At(16)), ERR_UNSUPPORTED, "256-byte"),
@@ -126,8 +127,9 @@ def test_workspace_bytes_depend_on_no_device_data():
                 for figure in (D.paged_select_workspace_bytes, D.paged_sparse_attention_workspace_bytes):
                     n = figure(p, b, s)
                     assert n > 0 and n % 256 == 0
-    # a row of scores for every token and KV head, as wide as the table
-    assert D.paged_select_workspace_bytes(pages(max_pages=100), blocks(), step()) >= 2 * 4 * 100 * 4
+    # a row of scores for every token and KV head, as wide as the table, where a second kernel reads them
+    assert D.paged_select_workspace_bytes(pages(max_pages=100), blocks(), step(total_new=8, max_new=4)) >= 8 * 4 * 100 * 4
+    assert D.paged_select_workspace_bytes(pages(max_pages=100), blocks(), step()) == 256
 
 
 def test_the_largest_descriptors():
