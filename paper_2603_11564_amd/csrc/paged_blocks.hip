@@ -33,24 +33,38 @@ struct BoundsParams {
   int32_t block_shift, max_rows;
 };
 
-// A wave has a block: 16 lanes to a row, eight channels to a lane, four rows at a time; the four meet at the end.
-template <int FMT>
+// Two bf16 as whole numbers of 16 bits that sort as they do, and back.  An infinity and what is no number lie past all others, at both ends.
+__device__ __forceinline__ unsigned sortable(unsigned x) {
+  return x ^ (__builtin_bit_cast(unsigned, __builtin_bit_cast(s16x2, x) >> (short)15) & 0x7fff7fffu);
+}
+__device__ __forceinline__ unsigned upper_of(unsigned a, unsigned b) {
+  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(s16x2, a), __builtin_bit_cast(s16x2, b)));
+}
+__device__ __forceinline__ unsigned lower_of(unsigned a, unsigned b) {
+  return __builtin_bit_cast(unsigned, __builtin_elementwise_min(__builtin_bit_cast(s16x2, a), __builtin_bit_cast(s16x2, b)));
+}
+
+// 16 lanes have a row, eight channels to a lane.  SHARED: a wave has a block, four rows at a time, which meet at the end; else four blocks, one to 16 lanes, so that
+// what a block costs beside its rows is shared by four.  Keys are compared as whole numbers, two to an instruction (a float to an instruction: 8 layers of
+// 32768 rows in blocks of 64 in 8 and in 4 bits 62 us, now 58 and 42).
+template <int FMT, bool SHARED>
 __global__ __launch_bounds__(256) void paged_bounds_kernel(BoundsParams p) {
   touch_args<sizeof(BoundsParams)>();
   const int lane = threadIdx.x & 63, ch = lane & 15, part = lane >> 4;
   const int layer = blockIdx.y / p.pool.n_kv_heads, head = blockIdx.y - layer * p.pool.n_kv_heads, seq = blockIdx.z;
   const int first = p.first == nullptr || p.first[seq] < 0 ? 0 : p.first[seq];
   const int64_t bound = (int64_t)first + p.max_rows, length = p.lengths[seq] < bound ? p.lengths[seq] : bound;
-  const int64_t block = (int64_t)(first >> p.block_shift) + blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if ((block + 1) << p.block_shift > length) return;
+  const int of_call = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t block = (int64_t)(first >> p.block_shift) + (SHARED ? of_call : 4 * of_call + part);
+  if ((block + 1) << p.block_shift > length) return;  // (16 lanes agree)
   const int64_t row0 = find_row(p.pool, layer, seq, head, block << p.block_shift);
   if (row0 < 0) return;
-  float hi[8], lo[8];
-  unsigned largest = 0;  // of the magnitudes, infinities and NaN among them
+  u32x4 hi, lo;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) hi[i] = -INFINITY, lo[i] = INFINITY;
-#pragma unroll 4
-  for (int r = part; r < 1 << p.block_shift; r += 4) {
+  for (int i = 0; i < 4; ++i) hi[i] = 0x80008000u, lo[i] = 0x7fff7fffu;
+  constexpr int kStep = SHARED ? 4 : 1;
+#pragma unroll(SHARED ? 4 : 8)
+  for (int r = SHARED ? part : 0; r < 1 << p.block_shift; r += kStep) {
     const int64_t row = row0 + r;
     u32x4 x;
     if constexpr (FMT == kBf16) {
@@ -66,35 +80,44 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(BoundsParams p) {
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float a = __uint_as_float(x[i] << 16), b = __uint_as_float(x[i] & 0xffff0000u);
-      hi[2 * i] = fmaxf(hi[2 * i], a), lo[2 * i] = fminf(lo[2 * i], a);
-      hi[2 * i + 1] = fmaxf(hi[2 * i + 1], b), lo[2 * i + 1] = fminf(lo[2 * i + 1], b);
-      largest = larger(largest, larger_magnitude(x[i]));
+      const unsigned whole = sortable(x[i]);
+      hi[i] = upper_of(hi[i], whole), lo[i] = lower_of(lo[i], whole);
     }
   }
+  unsigned largest = 0;  // of the magnitudes
 #pragma unroll
-  for (int d = 16; d < 64; d *= 2) {
+  for (int i = 0; i < 4; ++i) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], d, 64));
-      lo[i] = fminf(lo[i], __shfl_xor(lo[i], d, 64));
+    for (int d = 16; SHARED && d < 64; d *= 2) {
+      hi[i] = upper_of(hi[i], (unsigned)__shfl_xor((int)hi[i], d, 64));
+      lo[i] = lower_of(lo[i], (unsigned)__shfl_xor((int)lo[i], d, 64));
     }
+    hi[i] = sortable(hi[i]), lo[i] = sortable(lo[i]);
+    largest = larger(largest, larger(larger_magnitude(hi[i]), larger_magnitude(lo[i])));
   }
-  largest = wave_reduce<OpMax>(largest);
+  largest = larger(largest, dpp<kRor1>(largest));  // (of the 16 lanes that have a row)
+  largest = larger(largest, dpp<kRor2>(largest));
+  largest = larger(largest, dpp<kRor4>(largest));
+  largest = larger(largest, dpp<kRor8>(largest));
   const bool bad = largest >= 0x7f80u;
-  const int unit = unit_byte(largest);
+  const int unit = unit_byte(bad ? 0 : largest);
   const float per = power_of_two(254 - unit);
   const int64_t at = row0 >> p.block_shift;
-  // (the lanes of part 0 store the upper bounds, those of part 1 the lower ones)
-  unsigned w[2] = {0, 0};
+  // (of a block that a wave shares the lanes of part 0 store the upper bounds, those of part 1 the lower ones)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = part == 0 ? ceilf(hi[i] * per) : floorf(lo[i] * per);
-    const int whole = bad ? 0 : (int)fminf(fmaxf(x, -127.0f), 127.0f);
-    w[i >> 2] |= ((unsigned)whole & 255u) << (8 * (i & 3));
+  for (int side = 0; side < (SHARED ? 1 : 2); ++side) {
+    const bool upper = SHARED ? part == 0 : side == 0;
+    u32x2 w = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const unsigned two = upper ? hi[i >> 1] : lo[i >> 1];
+      const float y = __uint_as_float(i & 1 ? two & 0xffff0000u : two << 16) * per, x = upper ? ceilf(y) : floorf(y);
+      const int whole = bad ? 0 : (int)fminf(fmaxf(x, -127.0f), 127.0f);
+      w[i >> 2] |= ((unsigned)whole & 255u) << (8 * (i & 3));
+    }
+    if (!SHARED || part < 2) *reinterpret_cast<u32x2*>(p.bounds + at * (2 * kHeadDim) + (upper ? 0 : kHeadDim) + ch * 8) = w;
   }
-  if (part < 2) *reinterpret_cast<u32x2*>(p.bounds + at * (2 * kHeadDim) + part * kHeadDim + ch * 8) = u32x2{w[0], w[1]};
-  if (lane == 0) p.scales[at] = (uint8_t)(bad ? 255 : unit);
+  if ((SHARED ? lane : ch) == 0) p.scales[at] = (uint8_t)(bad ? 255 : unit);
 }
 
 // ---- dapq_paged_select ----------------------------------------------------------------------------------------------------
@@ -168,90 +191,93 @@ __device__ __forceinline__ Bin find_bin(const unsigned* bins, unsigned want, int
   return {bin, rest, (unsigned)__builtin_amdgcn_readlane((int)x[0], l)};
 }
 
-// The n_select largest keys of a token and KV head, of equal ones the first, in order.  A workgroup has the keys in registers, REGS times four in a
-// row to a thread.  The range that scores take is cut into 256 bins, then the bin that the last kept key lies in, until all of a bin is kept or it
-// is one key; every wave reads the bins by itself, so that a round is one barrier.
+// The cut of a token's keys.  The range that scores take is cut into 256 bins, then the bin that the last kept key lies in, until all of a bin is kept or it is
+// one key; every wave reads the bins by itself, so that a round is one barrier.  each(f) calls f with each of a thread's keys.
+template <int WAVES>
+struct CutLds {
+  __attribute__((aligned(16))) unsigned bins[4][256];
+  unsigned range[WAVES][4];  // of a wave: least and largest key, keys, ends
+};
+template <int WAVES, typename EACH>
+__device__ __forceinline__ Cut find_cut(const SelectParams& p, CutLds<WAVES>& lds, EACH each) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (tid < 256) lds.bins[i][tid] = 0;
+  unsigned low = kEndBlock, high = 0, n = 0, ends = 0;
+  each([&](unsigned x) {
+    n += x != kNoBlock;
+    ends += x == kEndBlock;
+    low = x != kNoBlock && x < low ? x : low;
+    high = x != kEndBlock && x > high ? x : high;
+  });
+  low = wave_reduce<OpMin>(low);
+  high = wave_reduce<OpMax>(high);
+  n = wave_sum(n);
+  ends = wave_sum(ends);
+  if (lane == 0) {
+    lds.range[wave][0] = low;
+    lds.range[wave][1] = high;
+    lds.range[wave][2] = n;
+    lds.range[wave][3] = ends;
+  }
+  __syncthreads();
+  n = ends = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    low = low < lds.range[w][0] ? low : lds.range[w][0];
+    high = larger(high, lds.range[w][1]);
+    n += lds.range[w][2];
+    ends += lds.range[w][3];
+  }
+  low = (unsigned)uniform((int)low), high = (unsigned)uniform((int)high);
+  if (n <= (unsigned)p.n_select) return {kNoBlock, 0};  // all
+  unsigned want = (unsigned)p.n_select - (unsigned)uniform((int)ends);
+  if (want == 0) return {kEndBlock - 1, 0};
+  // keys from `low` on, below low + 2^bits, in bins of 2^shift
+  int shift = high - low < 256u ? 0 : 24 - __builtin_clz(high - low);
+  int bits = 32;
+  for (int round = 0;; ++round) {
+    each([&](unsigned k) {
+      const unsigned x = k - low;
+      if (k != kNoBlock && k != kEndBlock && k >= low && (bits == 32 || x >> bits == 0)) atomicAdd(&lds.bins[round][x >> shift], 1u);
+    });
+    __syncthreads();
+    const Bin bin = find_bin(lds.bins[round], want, lane);
+    low += bin.at << shift;
+    want = bin.want;
+    if (bin.entries == want) return {low - 1, 0};  // the whole bin
+    if (shift == 0) return {low, want};
+    bits = shift;
+    shift = shift > 8 ? shift - 8 : 0;
+  }
+}
+
+// The n_select largest keys of a token and KV head, of equal ones the first, in order.  A workgroup has the keys in registers, REGS times four in a row to a thread.
 template <int WAVES, int REGS>
 struct Choice {
   static constexpr int kTurn = 256 * WAVES;  // keys that the workgroup takes at a time
   static_assert(WAVES * REGS <= 64, "a lane for the sum of each");
   struct Lds {
-    __attribute__((aligned(16))) unsigned bins[4][256];
-    unsigned range[WAVES][4];  // of a wave: least and largest key, keys, ends
+    CutLds<WAVES> cut;
     unsigned sums[WAVES * REGS];
   };
   // k: this thread's keys kTurn * r + 4 * tid .. + 3; row: layer, token and head as idx has them
   static __device__ __forceinline__ void run(const SelectParams& p, Lds& lds, u32x4 (&k)[REGS], int blocks, int64_t row) {
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (tid < 256) lds.bins[i][tid] = 0;
-    unsigned low = kEndBlock, high = 0, n = 0, ends = 0;
+    for (int r = 0; r < REGS; ++r)
 #pragma unroll
-    for (int r = 0; r < REGS; ++r) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 4; ++j)
         if (kTurn * r + 4 * tid + j >= blocks) k[r][j] = kNoBlock;
-        const unsigned x = k[r][j];
-        n += x != kNoBlock;
-        ends += x == kEndBlock;
-        low = x != kNoBlock && x < low ? x : low;
-        high = x != kEndBlock && x > high ? x : high;
+    const Cut cut = find_cut<WAVES>(p, lds.cut, [&](auto f) {
+#pragma unroll
+      for (int r = 0; r < REGS; ++r) {
+        if (r > 0 && kTurn * r >= blocks) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f(k[r][j]);
       }
-    }
-    low = wave_reduce<OpMin>(low);
-    high = wave_reduce<OpMax>(high);
-    n = wave_sum(n | ends << 16);  // (of a wave no more than 64 x 4 x REGS)
-    if (lane == 0) {
-      lds.range[wave][0] = low;
-      lds.range[wave][1] = high;
-      lds.range[wave][2] = n & 0xffffu;
-      lds.range[wave][3] = n >> 16;
-    }
-    __syncthreads();
-    n = ends = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      low = low < lds.range[w][0] ? low : lds.range[w][0];
-      high = larger(high, lds.range[w][1]);
-      n += lds.range[w][2];
-      ends += lds.range[w][3];
-    }
-    low = (unsigned)uniform((int)low), high = (unsigned)uniform((int)high);
-    Cut cut = {kNoBlock, 0};  // all
-    if (n > (unsigned)p.n_select) {
-      unsigned want = (unsigned)p.n_select - (unsigned)uniform((int)ends);
-      if (want == 0) {
-        cut.least = kEndBlock - 1;
-      } else {
-        // keys from `low` on, below low + 2^bits, in bins of 2^shift
-        int shift = high - low < 256u ? 0 : 24 - __builtin_clz(high - low);
-        int bits = 32;
-        for (int round = 0;; ++round) {
-#pragma unroll
-          for (int r = 0; r < REGS; ++r)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const unsigned x = k[r][j] - low;
-              if (k[r][j] != kNoBlock && k[r][j] != kEndBlock && k[r][j] >= low && (bits == 32 || x >> bits == 0)) atomicAdd(&lds.bins[round][x >> shift], 1u);
-            }
-          __syncthreads();
-          const Bin bin = find_bin(lds.bins[round], want, lane);
-          low += bin.at << shift;
-          want = bin.want;
-          if (bin.entries == want) {  // the whole bin
-            cut = {low - 1, 0};
-            break;
-          }
-          if (shift == 0) {
-            cut = {low, want};
-            break;
-          }
-          bits = shift;
-          shift = shift > 8 ? shift - 8 : 0;
-        }
-      }
-    }
+    });
     // in order, before a thread's keys: above the cut in the low half, equal to it in the high one
     unsigned upto[REGS];
 #pragma unroll
@@ -508,68 +534,54 @@ __global__ __launch_bounds__(64 * WAVES) void paged_choose_kernel(SelectParams p
   C::run(p, lds, k, blocks, blockIdx.x);
 }
 
-// The same of any number of keys, read again from memory for every eight bits of the smallest one that is kept.
-__global__ __launch_bounds__(256) void paged_choose_long_kernel(SelectParams p) {
+// The same of any number of keys, read again from memory for every round (25000 blocks LONGFIG).
+constexpr int kLongWaves = 16;
+__global__ __launch_bounds__(64 * kLongWaves) void paged_choose_long_kernel(SelectParams p) {
   touch_args<sizeof(SelectParams)>();
-  __shared__ __attribute__((aligned(16))) unsigned bins[4][256];
-  __shared__ unsigned sums[2][4];
+  constexpr int kTurn = 256 * kLongWaves;
+  __shared__ CutLds<kLongWaves> lds;
+  __shared__ unsigned sums[2][kLongWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int row = blockIdx.x / p.pool.n_kv_heads;  // layer * total_new + token
   int seq, t;
   if (!find_token(p.cu_new, p.batch, p.each_new, p.max_new, row % p.total_new, lane, &seq, &t)) return;
   const int blocks = uniform(blocks_seen(p, p.lengths[seq], t));
   const unsigned* keys = p.keys + (int64_t)blockIdx.x * p.stride;
+  auto four = [&](int i) {  // (a row has room for whole tiles, of which the last may hold keys past `blocks`: no blocks)
+    return i < blocks ? *reinterpret_cast<const u32x4*>(keys + i) : u32x4{kNoBlock, kNoBlock, kNoBlock, kNoBlock};
+  };
+  const Cut cut = find_cut<kLongWaves>(p, lds, [&](auto f) {
+#pragma unroll 4
+    for (int i = 4 * tid; i < blocks; i += kTurn) {
+      const u32x4 k = four(i);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) bins[i][tid] = 0;
-  __syncthreads();
-  Cut cut = {0, 0};
-  unsigned want = (unsigned)p.n_select;
-  for (int round = 0; round < 4; ++round) {
-    const int shift = 24 - 8 * round;
-    for (int i = tid; i < blocks; i += 256) {
-      const unsigned k = keys[i];
-      if (k != kNoBlock && (round == 0 || (k ^ cut.least) >> (shift + 8) == 0)) atomicAdd(&bins[round][(k >> shift) & 255u], 1u);
+      for (int j = 0; j < 4; ++j) f(i + j < blocks ? k[j] : kNoBlock);
     }
-    __syncthreads();
-    if (round == 0) {
-      unsigned all = bins[0][4 * lane] + bins[0][4 * lane + 1] + bins[0][4 * lane + 2] + bins[0][4 * lane + 3];
-      all = wave_sum(all);
-      if (all <= want) {  // (the same in all waves)
-        want = 0;
-        break;
-      }
-    }
-    const Bin bin = find_bin(bins[round], want, lane);
-    cut.least |= bin.at << shift;
-    want = bin.want;
-  }
-  cut.equal = want;
+  });
   int32_t* out = p.idx + (int64_t)blockIdx.x * p.n_select;
   unsigned above = 0, equal = 0;  // so far
-  for (int i0 = 0, turn = 0; i0 < blocks; i0 += 1024, turn ^= 1) {
-    unsigned k[4];
+  u32x4 next = four(4 * tid);
+  for (int i0 = 0, turn = 0; i0 < blocks; i0 += kTurn, turn ^= 1) {
+    u32x4 k = next;
+    next = four(i0 + kTurn + 4 * tid);
     unsigned both = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int i = i0 + 4 * tid + j;
-      k[j] = i < blocks ? keys[i] : kNoBlock;
-      both += (unsigned)(k[j] > cut.least) + ((unsigned)(k[j] == cut.least) << 16);
+      if (i0 + 4 * tid + j >= blocks) k[j] = kNoBlock;
+      both += (unsigned)(k[j] > cut.least) + ((unsigned)(k[j] == cut.least && k[j] != kNoBlock) << 16);
     }
     const unsigned upto = wave_scan<OpAdd>(both);
     if (lane == 63) sums[turn][wave] = upto;
     __syncthreads();  // (the sums of the turn before last are overwritten behind it)
-    unsigned all = 0, before = upto - both;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      before += w < wave ? sums[turn][w] : 0;
-      all += sums[turn][w];
-    }
+    const unsigned sum = lane < kLongWaves ? sums[turn][lane] : 0, scan = wave_scan<OpAdd>(sum);
+    const unsigned all = (unsigned)__builtin_amdgcn_readlane((int)scan, 63), before = upto - both + (unsigned)__builtin_amdgcn_readlane((int)(scan - sum), wave);
     unsigned a = above + (before & 0xffffu), e = equal + (before >> 16);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (k[j] > cut.least || (k[j] == cut.least && e < cut.equal)) out[a + (e < cut.equal ? e : cut.equal)] = i0 + 4 * tid + j;
+      const bool same = k[j] == cut.least && k[j] != kNoBlock;
+      if (k[j] > cut.least || (same && e < cut.equal)) out[a + (e < cut.equal ? e : cut.equal)] = i0 + 4 * tid + j;
       a += k[j] > cut.least;
-      e += k[j] == cut.least;
+      e += same;
     }
     above += all & 0xffffu;
     equal += all >> 16;
@@ -653,9 +665,15 @@ extern "C" DAPQ_API int dapq_paged_bounds(const dapq_pages* pages, const dapq_bl
   p.block_shift = __builtin_ctz((unsigned)blocks->block_rows);
   p.max_rows = max_rows;
   const int64_t all = most_blocks(pages, blocks), most = ((int64_t)max_rows + blocks->block_rows - 1) / blocks->block_rows;
-  const int64_t groups = ((most < all ? most : all) + 3) / 4;
+  // 8 layers of 32768 rows, us, a block of 16 rows shared by a wave / not, of 32, of 64: bf16 106 / 113, 101 / 108, 99 / 99; in 8 bits 85 / 62, 69 / 65, 58 / 57; in 4 bits
+  // 78 / 42, 53 / 35, 42 / 32, but 64 blocks of 64 rows 4.2 / 6.6.  In bf16 bytes bound both, and rows that follow each other are read at once by the first.
+  const bool shared = pages->format == DAPQ_PAGES_BF16 || blocks->block_rows > 32;
+  const int of_group = shared ? 4 : 16;  // blocks
+  const int64_t groups = ((most < all ? most : all) + of_group - 1) / of_group;
   DAPQ_REQUIRE(groups * 256 < (int64_t)1 << 32, DAPQ_ERR_UNSUPPORTED, "max_rows (%d) is too large", max_rows);
-  auto kernel = pages->format == DAPQ_PAGES_BF16 ? paged_bounds_kernel<kBf16> : (pages->format == DAPQ_PAGES_FP4 ? paged_bounds_kernel<kFp4> : paged_bounds_kernel<kE4m3>);
+  auto kernel = pages->format == DAPQ_PAGES_BF16 ? paged_bounds_kernel<kBf16, true>
+                : pages->format == DAPQ_PAGES_FP4 ? (shared ? paged_bounds_kernel<kFp4, true> : paged_bounds_kernel<kFp4, false>)
+                                                  : (shared ? paged_bounds_kernel<kE4m3, true> : paged_bounds_kernel<kE4m3, false>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)(pages->n_layers * pages->n_kv_heads), (unsigned)pages->batch), dim3(256), 0,
                      static_cast<hipStream_t>(stream), p);
   DAPQ_HIP_LAUNCH_CHECK("paged_bounds_kernel");
@@ -720,8 +738,10 @@ extern "C" DAPQ_API int dapq_paged_select(const dapq_pages* pages, const dapq_bl
   const unsigned rows = (unsigned)((int64_t)p.items * p.total_new);
   if (plan.stride <= 1024) hipLaunchKernelGGL((paged_choose_kernel<4, 1>), dim3(rows), dim3(256), 0, on, p);
   else if (plan.stride <= 2048) hipLaunchKernelGGL((paged_choose_kernel<4, 2>), dim3(rows), dim3(256), 0, on, p);
-  else if (plan.stride <= 16384) hipLaunchKernelGGL((paged_choose_kernel<16, 4>), dim3(rows), dim3(1024), 0, on, p);
-  else hipLaunchKernelGGL(paged_choose_long_kernel, dim3(rows), dim3(256), 0, on, p);
+  else if (plan.stride <= 4096) hipLaunchKernelGGL((paged_choose_kernel<4, 4>), dim3(rows), dim3(256), 0, on, p);
+  else if (plan.stride <= 8192) hipLaunchKernelGGL((paged_choose_kernel<8, 4>), dim3(rows), dim3(512), 0, on, p);
+  else if (plan.stride <= 16384) hipLaunchKernelGGL((paged_choose_kernel<8, 8>), dim3(rows), dim3(512), 0, on, p);
+  else hipLaunchKernelGGL(paged_choose_long_kernel, dim3(rows), dim3(64 * kLongWaves), 0, on, p);
   DAPQ_HIP_LAUNCH_CHECK("paged_choose_kernel");
   return DAPQ_OK;
 }

@@ -193,6 +193,27 @@ def test_numbers_of_blocks(n_select):
         check_choice(cache, b, [rows - 1], [1], normal_bits(rng, 1, 1, 4, 128), n_select, 0, 1)
 
 
+@pytest.mark.parametrize("blocks,new", [(60, 1), (300, 1), (300, 2), (2100, 1), (2100, 2)])
+def test_many_items(blocks, new):
+    """A workgroup scores all blocks of an item and chooses: tables of up to 256, 2048 and 8192 blocks, sequences of all lengths in them."""
+    rng = np.random.default_rng(blocks + new)
+    lengths = [16 * blocks - 5 - new] + [int(n) for n in rng.integers(1, 900, 32)]
+    lengths[20] = 0
+    cache = Cache(rng, "bf16", 1, 8, 16, [n + new for n in lengths]).to_device()
+    b = Bounds(cache, 16).random(rng).to_device()
+    check_choice(cache, b, lengths, [new] * 33, normal_bits(rng, 1, 33 * new, 32, 128), 9, 1, 2, ragged=False)
+
+
+@pytest.mark.parametrize("rows,wide", [(500, 17000), (66000, 2000), (131000, 1), (270000, 1)])
+def test_very_many_blocks(rows, wide):
+    """Tables of more than 4096, 8192 and 16384 blocks, the last of which are read again for every round of a choice; all alike in a second go."""
+    rng = np.random.default_rng(98)
+    cache = Cache(rng, "bf16", 1, 1, 16, [rows], extra_entries=wide).to_device()
+    for distinct in (True, False):
+        b = Bounds(cache, 16).random(rng, distinct).to_device()
+        check_choice(cache, b, [rows - 3], [3], normal_bits(rng, 1, 3, 2, 128), 300, 2, 1, ragged=False)
+
+
 def test_selection_with_pages_missing():
     rng = np.random.default_rng(91)
     lengths, new = [500, 200, 64, 20], [1, 3, 2, 1]
