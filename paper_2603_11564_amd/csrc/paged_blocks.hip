@@ -393,7 +393,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
       for (int i = 0; i < kAhead; ++i) fetch(ring[i], tile0 + wave + i * WAVES, pages[i]);
       int page = pages[kAhead];
       for (int c = tid >> 8; c < here; c += WAVES / 4) {
-        if (c >= WAVES / 4) x = query(c);
+        const u32x4 next = query(c + WAVES / 4);
         unsigned largest = larger(larger(larger_magnitude(x[0]), larger_magnitude(x[1])), larger(larger_magnitude(x[2]), larger_magnitude(x[3])));
         largest = larger(largest, dpp<kRor1>(largest));
         largest = larger(largest, dpp<kRor2>(largest));
@@ -415,6 +415,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
         *reinterpret_cast<u32x2*>(at) = up;
         *reinterpret_cast<u32x2*>(at + 2048) = down;
         if (o == 0) units[c * 16 + col] = power_of_two(unit);
+        x = next;
       }
       __syncthreads();
       i32x4 own[4];  // kOne: the column tile's operand
@@ -534,7 +535,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_choose_kernel(SelectParams p
   C::run(p, lds, k, blocks, blockIdx.x);
 }
 
-// The same of any number of keys, read again from memory for every round (25000 blocks LONGFIG).
+// The same of any number of keys, read again from memory for every round (one choice of 25000 blocks 18 us).
 constexpr int kLongWaves = 16;
 __global__ __launch_bounds__(64 * kLongWaves) void paged_choose_long_kernel(SelectParams p) {
   touch_args<sizeof(SelectParams)>();
@@ -621,8 +622,8 @@ SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
     plan.lds += (int)key_bytes;
     plan.chunk = tiles;
   } else {
-    plan.chunk = (tiles * items + 1023) / 1024;
-    plan.chunk = plan.chunk < 4 ? 4 : (plan.chunk + 3) / 4 * 4;
+    plan.chunk = (tiles * items * plan.columns + 1023) / 1024;
+    plan.chunk = plan.chunk < 4 ? 4 : (plan.chunk < tiles ? (plan.chunk + 3) / 4 * 4 : (tiles + 3) / 4 * 4);
   }
   plan.chunks = (tiles + plan.chunk - 1) / plan.chunk;
   return plan;
