@@ -429,7 +429,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
       // where the keys of this lane's token, in the first column tile here, are written; of the next one `next` further on
       const int token0 = WIDE ? (int)t0 : c0 * each + (n >> log2);
       const int64_t next = WHOLE ? each * p.stride : (int64_t)each * p.pool.n_kv_heads * p.stride;
-      unsigned* const to0 = (WHOLE ? whole_keys + token0 * p.stride : p.keys + (((int64_t)layer * p.total_new + first + token0) * p.pool.n_kv_heads + head) * p.stride) + 4 * kg;
+      unsigned* const to0 = (WHOLE ? whole_keys + (n >> log2) * p.stride : p.keys + (((int64_t)layer * p.total_new + first + token0) * p.pool.n_kv_heads + head) * p.stride) + 4 * kg;
       const bool writes = (n & ((1 << log2) - 1)) == 0;
       auto use = [&](const Tile& tile, int k) {
         // 16 lanes have brought in a block, whole lines of it; as operand a lane has its own: through LDS, with the 16 bytes of a block permuted by its number
@@ -495,19 +495,21 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
           if (k < tile1) use(ring[i], k);
         }
       }
-      if (WHOLE || COLUMNS != kOne) __syncthreads();
-    }
-  }
-  if constexpr (WHOLE) {
-    using C = Choice<WAVES, REGS>;
-    __shared__ typename C::Lds choice;
-    for (int t = 0; t < tokens; ++t) {
-      const unsigned* keys = whole_keys + t * p.stride;
-      const int blocks = blocks_seen(p, before, t);
-      u32x4 k[REGS];
+      if constexpr (WHOLE) {
+        using C = Choice<WAVES, REGS>;
+        __shared__ typename C::Lds choice;
+        __syncthreads();
+        for (int t = c0 * each; t < tokens && t < (c0 + 1) * each; ++t) {
+          const unsigned* keys = whole_keys + (t - c0 * each) * p.stride;
+          const int blocks = blocks_seen(p, before, t);
+          u32x4 k[REGS];
 #pragma unroll
-      for (int r = 0; r < REGS; ++r) k[r] = C::kTurn * r + 4 * tid < blocks ? *reinterpret_cast<const u32x4*>(keys + C::kTurn * r + 4 * tid) : u32x4{0, 0, 0, 0};
-      C::run(p, choice, k, blocks, ((int64_t)layer * p.total_new + first + t) * p.pool.n_kv_heads + head);
+          for (int r = 0; r < REGS; ++r) k[r] = C::kTurn * r + 4 * tid < blocks ? *reinterpret_cast<const u32x4*>(keys + C::kTurn * r + 4 * tid) : u32x4{0, 0, 0, 0};
+          C::run(p, choice, k, blocks, ((int64_t)layer * p.total_new + first + t) * p.pool.n_kv_heads + head);
+        }
+        return;  // (a workgroup has one column tile)
+      }
+      if (COLUMNS != kOne) __syncthreads();
     }
   }
 }
@@ -609,17 +611,23 @@ SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
   plan.columns = plan.cols_log2 > 4 ? most : (tiles_of_columns + plan.col_tiles - 1) / plan.col_tiles;
   plan.columns = plan.columns < 1 ? 1 : (plan.columns > 65535 ? 65535 : plan.columns);
   const int64_t items = (int64_t)pages->n_layers * pages->batch * pages->n_kv_heads;
-  plan.lds = plan.col_tiles * (kColTileBytes + 64);
-  // One kernel, a workgroup for all blocks of an item, or a kernel for chunks of them and one for the choice.  A workgroup takes 0.11 us a tile of its own, where the bytes
-  // of all take 0.75 ns (half of the table in use), and a second kernel some 3 us; tokens are chosen for one after the other.  Us, one kernel / two, 4 query heads of 8 KV
-  // heads, sequences x blocks: 1 x 128 6.5 / 8.9, 1 x 512 8.9 / 9.1, 1 x 2048 20.0 / 9.4, 8 x 512 9.1 / 9.8, 16 x 2048 20.9 / 21.4, 16 x 256..8192 65 / 42, 32 x 1024 16.0 / 20.5, 64 x
-  // 512 16.6 / 20.9, 64 x 2048 53 / 64; two tokens of 64 x 256 15.0 / 16.2, four of 16 x 512 17.1 / 12.2.
-  const int64_t key_bytes = most * plan.stride * 4;
-  plan.whole = plan.cols_log2 <= 4 && plan.col_tiles == 1 && most <= 2 && plan.stride <= 8192 && items < 1 << 20 && 0.11 * (double)tiles < 3.0 + 0.5 * 0.75e-3 * (double)(tiles * items);
+  // One kernel, a workgroup for all blocks of an item and a column tile of at most two tokens, or a kernel for chunks of blocks and one for the choice.  A workgroup takes 0.11 us a
+  // tile of its own, where the bytes of all take 0.75 ns (half of the table in use), and a second kernel some 3 us.  With several column tiles every workgroup reads the bounds, which
+  // pays while they are few.  Us, one kernel / two, 8 KV heads, 4 query heads a KV head, sequences x blocks: 1 x 128 6.5 / 8.9, 1 x 512 8.9 / 9.1, 1 x 2048 20.0 / 9.4, 8 x 512 9.1 / 9.8,
+  // 16 x 2048 20.9 / 21.4, 16 x 256..8192 65 / 42, 32 x 1024 16.0 / 20.5, 64 x 512 16.6 / 20.9, 64 x 2048 53 / 64, two tokens of 64 x 256 15.0 / 16.2; 8 query heads, four tokens of 16 x 512 12.3 /
+  // 13.5, of 64 x 64 11.2 / 14.6, of 64 x 256 25.4 / 18.1, eight of 64 x 64 18.5 / 21.0; 16 query heads, two tokens of 16 x 512 9.8 / 13.0, four of 32 x 512..2048 50 / 32.
+  const int64_t of_tile = most < each ? most : each;  // tokens of a column tile
+  const double all_bytes = 0.75e-3 * (double)(tiles * items);
+  plan.whole = plan.cols_log2 <= 4 && of_tile <= 2 && tiles_of_columns <= 16 && plan.stride <= 8192 && items < 1 << 20 && 0.11 * (double)tiles < 3.0 + 0.5 * all_bytes &&
+               (tiles_of_columns <= 1 || all_bytes * (double)tiles_of_columns < 9.0);
   plan.waves = plan.whole && plan.stride > 256 ? 8 : 4;
-  plan.lds += plan.waves * kColTileBytes;
   if (plan.whole) {
-    plan.lds += (int)key_bytes;
+    plan.col_tiles = 1;
+    plan.columns = tiles_of_columns < 1 ? 1 : tiles_of_columns;
+  }
+  plan.lds = plan.col_tiles * (kColTileBytes + 64) + plan.waves * kColTileBytes;
+  if (plan.whole) {
+    plan.lds += (int)(of_tile * plan.stride * 4);
     plan.chunk = tiles;
   } else {
     plan.chunk = (tiles * items * plan.columns + 1023) / 1024;

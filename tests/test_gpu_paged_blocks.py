@@ -204,6 +204,20 @@ def test_many_items(blocks, new):
     check_choice(cache, b, lengths, [new] * 33, normal_bits(rng, 1, 33 * new, 32, 128), 9, 1, 2, ragged=False)
 
 
+@pytest.mark.parametrize("group,new", [(8, 4), (8, 5), (16, 2), (16, 7), (4, 9), (5, 3), (12, 16)])
+def test_many_items_of_several_column_tiles(group, new):
+    """Two tokens of a column tile and fewer: a workgroup has one; sequences with fewer tokens than others."""
+    rng = np.random.default_rng(group * 100 + new)
+    lengths = [int(n) for n in rng.integers(0, 700, 20)]
+    tokens = [int(n) for n in rng.integers(0, new + 1, 20)]
+    tokens[4] = new
+    cache = Cache(rng, "bf16", 1, 4, 32, [n + new for n in lengths]).to_device()
+    b = Bounds(cache, 16).random(rng).to_device()
+    check_choice(cache, b, lengths, tokens, normal_bits(rng, 1, sum(tokens), 4 * group, 128), 6, 1, 1)
+    new_all = [new] * 20
+    check_choice(cache, b, lengths, new_all, normal_bits(rng, 1, 20 * new, 4 * group, 128), 6, 0, 1, ragged=False)
+
+
 @pytest.mark.parametrize("rows,wide", [(500, 17000), (66000, 2000), (131000, 1), (270000, 1)])
 def test_very_many_blocks(rows, wide):
     """Tables of more than 4096, 8192 and 16384 blocks, the last of which are read again for every round of a choice; all alike in a second go."""
