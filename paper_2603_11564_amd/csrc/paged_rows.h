@@ -623,6 +623,14 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(RowParams<S
     if (parts <= 1 || col >= s.tokens * p.group) return;
     first += ((int)from_lane(wave_scan<OpAdd>(own), seq & 63) - parts) * p.items + item * parts;
   }
+  constexpr bool kFew = EARLY >= 16;  // (no more parts than the lanes of a row, which meet without the LDS crossbar)
+  auto first16 = [](float x, auto op) {
+    x = op(x, __uint_as_float(dpp<kRor1>(__float_as_uint(x))));
+    x = op(x, __uint_as_float(dpp<kRor2>(__float_as_uint(x))));
+    x = op(x, __uint_as_float(dpp<kRor4>(__float_as_uint(x))));
+    x = op(x, __uint_as_float(dpp<kRor8>(__float_as_uint(x))));
+    return __uint_as_float((unsigned)uniform((int)__float_as_uint(x)));
+  };
   auto part = [&](int i) { return p.parts + (int64_t)(first + i) * Part<COLS>::kFloats; };
   float m = -INFINITY, sum = 0.0f;
   f32x2 o = {0.0f, 0.0f};
@@ -634,12 +642,14 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(RowParams<S
 #pragma unroll
     for (int i = 0; i < EARLY; ++i) early[i] = *reinterpret_cast<const f32x2*>(part(i0 + WAVES * (i < n ? i : n - 1)) + col * kHeadDim + 2 * lane);
     float top = r;
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    if constexpr (kFew) top = first16(top, [](float a, float b) { return fmaxf(a, b); });
+    else for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     const float moved = fmaxf(m, top);
     if (moved == -INFINITY) continue;
     const float f = __builtin_amdgcn_exp2f(r - moved), before = __builtin_amdgcn_exp2f(m - moved);  // (parts without a row: 0)
     w = f == 0.0f && r == -INFINITY ? 0.0f : w * f;
-    for (int d = 32; d > 0; d >>= 1) w += __shfl_xor(w, d, 64);
+    if constexpr (kFew) w = first16(w, [](float a, float b) { return a + b; });
+    else for (int d = 32; d > 0; d >>= 1) w += __shfl_xor(w, d, 64);
     sum = m == -INFINITY ? w : fmaf(sum, before, w);
     if (m != -INFINITY) o *= before;
     m = moved;
