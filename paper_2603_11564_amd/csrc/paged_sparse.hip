@@ -21,6 +21,8 @@ SparsePlan sparse_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
   const int64_t all = most_blocks(pages, blocks), rows = (blocks->n_select < all ? blocks->n_select : all) * blocks->block_rows;
   const int64_t tiles = (rows + kTile - 1) / kTile;
   plan.tiles = (int)(((int64_t)blocks->n_select * blocks->block_rows + kTile - 1) / kTile);  // (up to 2^17: parts_each times it stays below 2^31)
+  // Parts for as many workgroups as the chip holds at once, but of no fewer tiles than a workgroup has waves.  8 KV heads of one token, us with parts of
+  // 2 / 4 / 8 tiles at least: 2048 rows of 4 query heads 9.8 / 9.3 / 10.5, of 8 query heads 10.2 / 10.2 / 11.4, 4096 rows 12.7 / 10.9 / 12.0.
   const int64_t resident = plan.cols == 32 ? 512 : 768, items = plan.items * plan.chunks;
   int64_t parts = items > 0 ? resident / items : 1;
   if (parts > tiles / kRowWaves) parts = tiles / kRowWaves;
@@ -40,7 +42,9 @@ int launch_sparse(const SparseParams& p, const SparsePlan& plan, hipStream_t str
   DAPQ_HIP_LAUNCH_CHECK("paged_rows_kernel");
   if (SPLIT) {
     const unsigned cols = (unsigned)(p.group < kCols ? p.group : kCols);
-    if (plan.items < 128 && plan.parts > 16) hipLaunchKernelGGL((paged_join_kernel<kCols, kJoinWaves, true>), dim3((unsigned)plan.items, cols, (unsigned)plan.chunks), dim3(64 * kJoinWaves), 0, stream, p);
+    // Up to 16 parts (always so with 128 items, which leave 6 to each) are joined by a wave, whose first 16 lanes hold their weights.  More take eight waves:
+    // 8 KV heads, us, one wave / eight, 32 parts 16.7 / 10.4, 96 parts 44 / 21.
+    if (plan.parts > 16) hipLaunchKernelGGL((paged_join_kernel<kCols, kJoinWaves, true>), dim3((unsigned)plan.items, cols, (unsigned)plan.chunks), dim3(64 * kJoinWaves), 0, stream, p);
     else hipLaunchKernelGGL((paged_join_kernel<kCols, 1, true, 16>), dim3((unsigned)plan.items, (cols + kJoinWaves - 1) / kJoinWaves, (unsigned)plan.chunks), dim3(64 * kJoinWaves), 0, stream, p);
     DAPQ_HIP_LAUNCH_CHECK("paged_join_kernel");
   }
