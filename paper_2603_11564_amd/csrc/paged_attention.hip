@@ -80,7 +80,7 @@ int check_attention(const dapq_pages* pages, const dapq_step* step) {
   DAPQ_REQUIRE(step->scale <= 0x1p126f && step->softcap <= 0x1p126f, DAPQ_ERR_UNSUPPORTED, "scale (%g) or softcap (%g) exceeds 2^126", step->scale, step->softcap);
   const double ratio = step->softcap > 0.0f ? (double)step->scale / step->softcap : 1.0;
   DAPQ_REQUIRE(ratio >= 0x1p-110 && ratio <= 0x1p110, DAPQ_ERR_UNSUPPORTED, "scale (%g) / softcap (%g) must be from 2^-110 to 2^110", step->scale, step->softcap);
-  DAPQ_REQUIRE(step->total_new * step->n_q_heads < (int64_t)1 << 31, DAPQ_ERR_UNSUPPORTED,
+  DAPQ_REQUIRE(step->n_q_heads <= 65535 && step->total_new * step->n_q_heads < (int64_t)1 << 31, DAPQ_ERR_UNSUPPORTED,
                "n_q_heads (%d) exceeds 65535, or total_new (%lld) query rows of all heads 2^31", step->n_q_heads, (long long)step->total_new);
   return DAPQ_OK;
 }

@@ -9,7 +9,7 @@ import paper_2603_11564_amd as D
 from oracle import blocks_oracle as BO
 from oracle import dapq_oracle as O
 from paper_2603_11564_amd import binding
-from test_paged_host import A, ERR_INVALID, ERR_UNSUPPORTED, ERR_WORKSPACE, At, BAD_PAGES, fp4, pages, step
+from test_paged_host import A, ERR_INVALID, ERR_UNSUPPORTED, ERR_WORKSPACE, At, BAD_PAGES, attention, fp4, pages, step
 
 N = None
 
@@ -94,6 +94,16 @@ def test_refusals(call, code, message):
     with pytest.raises(D.DapqError, match=message) as e:
         call()
     assert e.value.code == code
+
+
+@pytest.mark.parametrize("call,figure", [(lambda s: attention(s=s), lambda s: D.paged_attention_workspace_bytes(pages(), s)),
+                                         (lambda s: sparse(s=s), lambda s: D.paged_sparse_attention_workspace_bytes(pages(), blocks(), s))], ids=["attention", "sparse"])
+def test_more_query_heads_than_a_launch_has_are_refused(call, figure):
+    for heads in (65536, 1 << 30):
+        with pytest.raises(D.DapqError, match="exceeds 65535") as e:
+            call(step(n_q_heads=heads))
+        assert e.value.code == ERR_UNSUPPORTED and figure(step(n_q_heads=heads)) == 0
+    assert figure(step(n_q_heads=65532)) > 0
 
 
 def test_nothing_to_do_is_no_error():
