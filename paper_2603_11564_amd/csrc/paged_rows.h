@@ -13,7 +13,7 @@ struct SparseParams : PagedAttentionParams {
   const int32_t *idx, *count;
   int32_t block_shift, n_select;
   int32_t parts_each;  // workgroups of an item
-  int32_t most_tiles;  // of n_select blocks
+  int32_t most_tiles;  // of n_select blocks, or of all that there are, if they are fewer
 };
 template <bool SPARSE>
 using RowParams = std::conditional_t<SPARSE, SparseParams, PagedAttentionParams>;
@@ -157,7 +157,8 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
     part = blockIdx.y;
     parts = p.parts_each;
     const int kept = p.count[blockIdx.x];
-    // parts are cut from the most rows that there may be, so that the first blocks are on their way before the count is known
+    // parts are cut from the most rows that there may be, so that the first blocks are on their way before the count is known; blocks named more than once may be
+    // more yet, which the last part has
     tile0 = uniform(p.most_tiles * part / parts);
     tile1 = uniform(p.most_tiles * (part + 1) / parts);
     blocks_of((tile0 + wave + (int64_t)kRowWaves * lane) * kTile);
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
     chosen_count = uniform(kept < 0 ? 0 : (kept < p.n_select ? kept : p.n_select));
     const int64_t rows = (int64_t)chosen_count << p.block_shift;
     s = {r, 1, before, (int)((rows + kTile - 1) / kTile)};
-    tile1 = tile1 < s.tiles ? tile1 : s.tiles;
+    tile1 = tile1 < s.tiles && part + 1 < parts ? tile1 : s.tiles;
   } else if constexpr (SPLIT) {
     Tiles t = tiles_of_64(p, 0, lane);
     int64_t total = from_lane(t.upto, 63);

@@ -20,7 +20,7 @@ SparsePlan sparse_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
   plan.items = (int64_t)pages->n_layers * step->total_new * pages->n_kv_heads;
   const int64_t all = most_blocks(pages, blocks), rows = (blocks->n_select < all ? blocks->n_select : all) * blocks->block_rows;
   const int64_t tiles = (rows + kTile - 1) / kTile;
-  plan.tiles = (int)(((int64_t)blocks->n_select * blocks->block_rows + kTile - 1) / kTile);  // (up to 2^17: parts_each times it stays below 2^31)
+  plan.tiles = (int)tiles;  // (up to 2^17: parts_each times it stays below 2^31)
   // Parts for as many workgroups as the chip holds at once, but of no fewer tiles than a workgroup has waves.  8 KV heads of one token, us with parts of
   // 2 / 4 / 8 tiles at least: 2048 rows of 4 query heads 9.8 / 9.3 / 10.5, of 8 query heads 10.2 / 10.2 / 11.4, 4096 rows 12.7 / 10.9 / 12.0.
   const int64_t resident = plan.cols == 32 ? 512 : 768, items = plan.items * plan.chunks;

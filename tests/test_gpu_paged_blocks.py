@@ -438,6 +438,16 @@ def test_a_block_named_twice_counts_twice():
     assert (np.abs(got[0, 0, 0] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -14 * np.abs(v).max()).all()
 
 
+@pytest.mark.parametrize("n_select", [37, 38, 39, 77, 300, 4096])
+def test_more_entries_than_the_table_has_blocks(n_select):
+    """Blocks of a table of 38, in any order and more than once, or few of them where there is room for many."""
+    rng = np.random.default_rng(74 + n_select)
+    cache = Cache(rng, "bf16", 1, 2, 16, [600, 20], extra_entries=0).fill(rng, [600, 20]).to_device()
+    idx = rng.integers(0, 38, (1, 2, 2, n_select)).astype(np.int32)
+    count = np.array([[[n_select, min(n_select, 38)], [n_select, 5]]], np.int32)
+    check_sparse(cache, [599, 19], [1, 1], normal_bits(rng, 1, 2, 8, 128), idx, count, 16)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("group,n_select", [(1, 6), (4, 6), (12, 6), (24, 6), (4, 70)])
 def test_what_is_not_finite(fmt, group, n_select):
