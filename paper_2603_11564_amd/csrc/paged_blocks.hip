@@ -473,17 +473,14 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
         u32x4 of_token = {0, 0, 0, 0};
 #pragma unroll 2
         for (int c = 0; c < here; ++c) {
-          i32x4 up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
+          i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            up = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], COLUMNS == kOne ? own[i] : operand(c, i), up, 0, 0, 0);
-            down = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[2 + i], COLUMNS == kOne ? own[2 + i] : operand(c, 2 + i), down, 0, 0, 0);
-          }
+          for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], COLUMNS == kOne ? own[i] : operand(c, i), sum, 0, 0, 0);
           const float unit = COLUMNS == kOne ? own_unit : units[c * 16 + n];
           u32x4 keys;
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            keys[v] = key_of((float)(up[v] + down[v]) * unit * factor[v]);
+            keys[v] = key_of((float)sum[v] * unit * factor[v]);
             of_token[v] = larger(of_token[v], keys[v]);
           }
           if (!WIDE) put(keys, c);
