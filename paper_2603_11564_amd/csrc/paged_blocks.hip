@@ -254,7 +254,7 @@ __device__ __forceinline__ Cut find_cut(const SelectParams& p, CutLds<WAVES>& ld
 }
 
 // The n_select largest keys of a token and KV head, of equal ones the first, in order.  A workgroup has the keys in registers, REGS times four in a row to a thread.
-// A chain of four barriers and, as a kernel, three trips to memory: 64 of 2048 for 8 items 4.8 us, for 1024 7.6, of 2063 for 12800 57 (of 8 KB each: 1.9 TB/s).
+// A chain of four barriers and, as a kernel, three trips to memory: 64 of 2048 for 8 items 4.8 us, for 1024 7.6, of 2063 for 12800 55 (of 8 KB each: 1.9 TB/s).
 template <int WAVES, int REGS>
 struct Choice {
   static constexpr int kTurn = 256 * WAVES;  // keys that the workgroup takes at a time
@@ -319,7 +319,7 @@ constexpr int kColTiles = 8, kColTileBytes = 4096;  // column tiles in LDS, at m
 // Bound by the bytes of the bounds where tokens are few: 64 sequences of 32768 rows, 8 KV heads, blocks of 16 (269 MB) 53 us with the choice (5.1 TB/s), of 4096..32768 rows
 // in blocks of 32 (73 MB) 20.  A workgroup brings the columns of some tokens into LDS as operands, then each wave takes tiles of 16 blocks.  16 lanes load a block, whole lines of
 // it, and the tile is turned in LDS: loaded as operands, 64 bytes of 16 blocks at a time, lines left the cache between their halves (22.6 us, with more tiles on their way 24 and 27).
-// Many tokens are bound by vector instructions, some 45 to a tile and 16 columns: 200 tokens of 8 sequences of 8192..32768 rows 65 us.
+// Many tokens are bound by a chain of some 40 vector instructions to a tile and 16 columns, and its waits: 200 tokens of 8 sequences of 8192..32768 rows 62 us.
 // COLUMNS: kOne: one column tile in all, whose operand stays in registers; kMany; kWide: a token has more than 16 query heads, and several column tiles.
 // REGS: of the Choice of the same workgroup, which has all tiles of the sequence and keeps their keys in LDS; 0: the keys go to the workspace.
 enum Columns { kOne, kMany, kWide };
