@@ -631,8 +631,8 @@ SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
     plan.lds += (int)(of_tile * plan.stride * 4);
     plan.chunk = tiles;
   } else {
-    // Chunks for some 1024 workgroups: four tokens of 32 sequences of 512..2048 blocks, scores with 512 / 768 / 1024 / 1536 / 2048 / 3072 workgroups 26.3 / 24.8 / 23.2 / 24.3 / 24.5 /
-    // 26.0 us.  No fewer than 4 tiles, one to a wave.
+    // Chunks for some 1024 workgroups: four tokens of 32 sequences of 512..2048 blocks, scores with 512 / 768 / 1024 / 1536 / 2048 workgroups 26.3 / 24.8 / 23.2 / 24.3 / 24.5 us.
+    // No fewer than 4 tiles, one to a wave.
     plan.chunk = (tiles * items * plan.columns + 1023) / 1024;
     plan.chunk = plan.chunk < 4 ? 4 : (plan.chunk < tiles ? (plan.chunk + 3) / 4 * 4 : (tiles + 3) / 4 * 4);
   }
