@@ -6,6 +6,8 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import paper_2603_11564_amd as D  # noqa: E402
+import test_gpu_paged_e4m3 as E4M3  # noqa: E402
+import test_gpu_paged_scales as SCALES  # noqa: E402
 from dapq_harness import Problem  # noqa: E402
 from oracle import blocks_oracle as BO  # noqa: E402
 from oracle import dapq_oracle as O  # noqa: E402
@@ -474,6 +476,30 @@ def test_what_is_not_finite(fmt, group, n_select):
     with np.errstate(invalid="ignore"):
         assert (np.abs(got - want) <= attention_bound(want, weighted, size, 1))[finite].all()
     assert finite[0, [0, 5, 7]].all() and not finite[0, [1, 2, 3, 4, 6]].all(axis=(1, 2)).any()
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "e4m3"])
+@pytest.mark.parametrize("group,n_select", [(1, 6), (4, 40), (12, 6), (24, 40)])
+def test_values_past_the_largest_scales(fmt, group, n_select):
+    """Groups of codes with infinite values among them: what the tokens see whose blocks have the row.  With queries of 0 every weight is 1, and a channel has one
+    such value."""
+    module = SCALES if fmt == "fp4" else E4M3
+    rng = np.random.default_rng(76 + group)
+    cache = Cache(rng, fmt, 1, 2, 32, [200]).fill(rng, [200])
+    for g, (row, byte) in enumerate(((5, 253), (45, 254), (102, 254), (104, 253))):
+        module.plant(rng, cache, "v", 1, row, g, byte, range(8) if fmt == "fp4" else range(0x70, 0x7f))
+    cache.to_device()
+    idx, count = np.full((1, 4, 2, n_select), -1, np.int32), np.full((1, 4, 2), n_select, np.int32)
+    idx[0, :, :, :6] = np.array([[0, 2, 6, 1, 3, 4], [6, 1, 3, 4, 5, 12], [0, 1, 2, 3, 4, 5], [6, 5, 4, 3, 2, 1]])[:, None]
+    q = np.zeros((1, 4, 2 * group, 128), np.uint16)
+    got = sparse(cache, [101], [4], q, idx, count, 16)              # token 0 sees row 101
+    with np.errstate(invalid="ignore", over="ignore"):
+        want, weighted, size = BO.sparse_attention(module.as_bf16(cache), cache.table, [101], [0, 4], 4, O.bf16_bits_to_f64(q), idx, count, 16, SCALE)
+        finite = np.isfinite(want)
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and (got[np.isinf(want)] == want[np.isinf(want)]).all()
+        assert (np.abs(got - want) <= attention_bound(want, weighted, size, 1))[finite].all()
+    inf = np.isinf(want[0, :, group:]).reshape(4, group, 4, 32).any((1, 3))
+    assert inf.tolist() == [[True, True, False, False], [False, False, True, False], [True, True, False, False], [False, True, True, True]]
 
 
 def test_extreme_scores():
