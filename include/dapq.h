@@ -424,8 +424,10 @@ int dapq_paged_bounds(const dapq_pages* pages, const dapq_blocks* blocks, const 
  *   q      device, bf16, rotated, as for dapq_paged_attention (the q strides of step)
  *   idx    out, int32 [n_layers][total_new][n_kv_heads][n_select]: blocks, ascending; entries past count are left as they were
  *   count  out, int32 [n_layers][total_new][n_kv_heads]; idx and count of tokens past max_new are left as they were
- *   workspace  device scratch of at least dapq_paged_select_workspace_bytes(pages, blocks, step), 256-byte aligned: scores of the blocks.  The figure depends
- *        on neither the lengths nor cu_new.
+ *   workspace  device scratch of at least dapq_paged_select_workspace_bytes(pages, blocks, step), 256-byte aligned: scores of the blocks, 4 bytes for every
+ *        token, KV head and block that the table has room for (a step of one token of 64 sequences, 8 KV heads, tables of 2048 blocks: 4 MB; 10000 tokens and 8192 blocks: 2.6 GB),
+ *        or 256 bytes where no step of that size needs it.  The figure depends on neither the lengths nor cu_new, be it NULL or not, and is enough for every step of
+ *        no more sequences, layers, KV heads and new tokens (total_new and max_new), and tables no wider, with as many query heads a KV head.
  * Uses the table of pages, all of blocks, and n_q_heads, max_new, total_new, cu_new, lengths and the q strides of step. */
 int dapq_paged_select(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, const void* q, int32_t* idx, int32_t* count,
                       void* workspace, size_t workspace_bytes, void* stream);
@@ -437,7 +439,8 @@ size_t dapq_paged_select_workspace_bytes(const dapq_pages* pages, const dapq_blo
  * of the blocks idx[layer][cu_new[seq] + t][kv_head][0 .. count - 1], in the format of dapq_paged_select.  An entry that is no block of the table has no rows;
  * blocks may stand in any order, and one that is named twice counts twice.  A count past n_select counts as n_select, a negative one as 0.
  *   q, out     as for dapq_paged_attention; 0 where no row is visible
- *   workspace  device scratch of at least dapq_paged_sparse_attention_workspace_bytes(pages, blocks, step), 256-byte aligned
+ *   workspace  device scratch of at least dapq_paged_sparse_attention_workspace_bytes(pages, blocks, step), 256-byte aligned; up to 8.5 MB.  The figure holds for
+ *        smaller steps as that of dapq_paged_select does
  * Uses block_rows and n_select of blocks (bounds and scales may be NULL), and what dapq_paged_attention uses of step, softcap too.  Sums, weights
  * and values that are not finite are as in dapq_paged_attention of few query rows.  The work is that of the chosen rows, read anew for every token: a
  * turn of many tokens behind a cache that is not many times longer than n_select * block_rows is done sooner by dapq_paged_attention (200 tokens over 64 blocks of 16

@@ -599,28 +599,41 @@ struct SelectPlan {
   bool whole;  // a workgroup scores all blocks of a sequence and KV head and chooses them
   int waves, lds;
 };
+int columns_log2(const dapq_pages* pages, const dapq_step* step) {
+  int log2 = 0;
+  while (1 << log2 < step->n_q_heads / pages->n_kv_heads) ++log2;
+  return log2;
+}
+int64_t column_tiles(int group, int cols_log2, int64_t most) {
+  const int64_t each = cols_log2 < 4 ? 16 >> cols_log2 : 1;
+  return cols_log2 > 4 ? (group + 15) / 16 : (most + each - 1) / each;
+}
+// One kernel, a workgroup for all blocks of an item and a column tile of at most two tokens, or a kernel for chunks of blocks and one for the choice; `most` new tokens of a
+// sequence, `items` sequences x KV heads x layers.  A workgroup takes 0.11 us a tile of its own, where the bytes of all take 0.75 ns (half of the table in use), and a second kernel
+// some 3 us.  With several column tiles every workgroup reads the bounds, which pays while they are few.  Us, one kernel / two, 8 KV heads, 4 query heads a KV head, sequences x blocks: 1 x 128 6.5 / 8.9, 1 x 512 8.9 / 9.1, 1 x 2048 20.0 / 9.4, 8 x 512 9.1 / 9.8,
+// 16 x 2048 20.9 / 21.4, 16 x 256..8192 65 / 42, 32 x 1024 16.0 / 20.5, 64 x 512 16.6 / 20.9, 64 x 2048 53 / 64, two tokens of 64 x 256 15.0 / 16.2; 8 query heads, four tokens of 16 x 512 12.3 /
+// 13.5, of 64 x 64 11.2 / 14.6, of 64 x 256 25.4 / 18.1, eight of 64 x 64 18.5 / 21.0; 16 query heads, two tokens of 16 x 512 9.8 / 13.0, four of 32 x 512..2048 50 / 32.
+// fewest: the items; or 1, to ask whether calls of fewer items are one kernel as well (fewer tokens and items meet all other conditions too).
+bool in_one_kernel(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, int64_t most, int64_t items, int64_t fewest) {
+  const int cols_log2 = columns_log2(pages, step);
+  const int64_t tiles = (most_blocks(pages, blocks) + 15) / 16, each = cols_log2 < 4 ? 16 >> cols_log2 : 1, of_tile = most < each ? most : each;  // tokens of a column tile
+  const int64_t col_tiles = column_tiles(step->n_q_heads / pages->n_kv_heads, cols_log2, most);
+  auto bytes_of = [&](int64_t n) { return 0.75e-3 * (double)(tiles * n); };
+  return cols_log2 <= 4 && of_tile <= 2 && col_tiles <= 16 && 16 * tiles <= 8192 && items < 1 << 20 && 0.11 * (double)tiles < 3.0 + 0.5 * bytes_of(fewest) &&
+         (col_tiles <= 1 || bytes_of(items) * (double)col_tiles < 9.0);
+}
 SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step) {
   SelectPlan plan;
   const int64_t tiles = (most_blocks(pages, blocks) + 15) / 16;
   plan.stride = 16 * tiles;
   const int group = step->n_q_heads / pages->n_kv_heads;
-  plan.cols_log2 = 0;
-  while (1 << plan.cols_log2 < group) ++plan.cols_log2;
-  const int64_t most = most_new(pages, step), each = plan.cols_log2 < 4 ? 16 >> plan.cols_log2 : 1;
-  const int64_t tiles_of_columns = plan.cols_log2 > 4 ? (group + 15) / 16 : (most + each - 1) / each;
+  plan.cols_log2 = columns_log2(pages, step);
+  const int64_t most = most_new(pages, step), tiles_of_columns = column_tiles(group, plan.cols_log2, most);
   plan.col_tiles = (int)(tiles_of_columns < kColTiles ? (tiles_of_columns < 1 ? 1 : tiles_of_columns) : kColTiles);
   plan.columns = plan.cols_log2 > 4 ? most : (tiles_of_columns + plan.col_tiles - 1) / plan.col_tiles;
   plan.columns = plan.columns < 1 ? 1 : (plan.columns > 65535 ? 65535 : plan.columns);
   const int64_t items = (int64_t)pages->n_layers * pages->batch * pages->n_kv_heads;
-  // One kernel, a workgroup for all blocks of an item and a column tile of at most two tokens, or a kernel for chunks of blocks and one for the choice.  A workgroup takes 0.11 us a
-  // tile of its own, where the bytes of all take 0.75 ns (half of the table in use), and a second kernel some 3 us.  With several column tiles every workgroup reads the bounds, which
-  // pays while they are few.  Us, one kernel / two, 8 KV heads, 4 query heads a KV head, sequences x blocks: 1 x 128 6.5 / 8.9, 1 x 512 8.9 / 9.1, 1 x 2048 20.0 / 9.4, 8 x 512 9.1 / 9.8,
-  // 16 x 2048 20.9 / 21.4, 16 x 256..8192 65 / 42, 32 x 1024 16.0 / 20.5, 64 x 512 16.6 / 20.9, 64 x 2048 53 / 64, two tokens of 64 x 256 15.0 / 16.2; 8 query heads, four tokens of 16 x 512 12.3 /
-  // 13.5, of 64 x 64 11.2 / 14.6, of 64 x 256 25.4 / 18.1, eight of 64 x 64 18.5 / 21.0; 16 query heads, two tokens of 16 x 512 9.8 / 13.0, four of 32 x 512..2048 50 / 32.
-  const int64_t of_tile = most < each ? most : each;  // tokens of a column tile
-  const double all_bytes = 0.75e-3 * (double)(tiles * items);
-  plan.whole = plan.cols_log2 <= 4 && of_tile <= 2 && tiles_of_columns <= 16 && plan.stride <= 8192 && items < 1 << 20 && 0.11 * (double)tiles < 3.0 + 0.5 * all_bytes &&
-               (tiles_of_columns <= 1 || all_bytes * (double)tiles_of_columns < 9.0);
+  plan.whole = in_one_kernel(pages, blocks, step, most, items, items);
   plan.waves = plan.whole && plan.stride > 256 ? 8 : 4;
   if (plan.whole) {
     plan.col_tiles = 1;
@@ -628,7 +641,8 @@ SelectPlan select_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
   }
   plan.lds = plan.col_tiles * (kColTileBytes + 64) + plan.waves * kColTileBytes;
   if (plan.whole) {
-    plan.lds += (int)(of_tile * plan.stride * 4);
+    const int64_t each = plan.cols_log2 < 4 ? 16 >> plan.cols_log2 : 1;
+    plan.lds += (int)((most < each ? most : each) * plan.stride * 4);
     plan.chunk = tiles;
   } else {
     // Chunks for some 1024 workgroups: four tokens of 32 sequences of 512..2048 blocks, scores with 512 / 768 / 1024 / 1536 / 2048 workgroups 26.3 / 24.8 / 23.2 / 24.3 / 24.5 us.
@@ -694,9 +708,11 @@ extern "C" DAPQ_API int dapq_paged_bounds(const dapq_pages* pages, const dapq_bl
 
 extern "C" DAPQ_API size_t dapq_paged_select_workspace_bytes(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step) {
   if (check_select(pages, blocks, step) != DAPQ_OK) return 0;
-  const int64_t rows = (int64_t)pages->n_layers * step->total_new * pages->n_kv_heads;
-  const SelectPlan plan = select_plan(pages, blocks, step);
-  return plan.whole ? 256 : align_up((size_t)(rows < 1 ? 1 : rows) * plan.stride * sizeof(unsigned), 256);
+  // Enough for every smaller step as well, however its tokens are packed: one of fewer items may take two kernels where this one takes one, whose keys are no more than these.
+  const int64_t most = step->max_new < step->total_new ? step->max_new : step->total_new, items = (int64_t)pages->n_layers * pages->batch * pages->n_kv_heads;
+  if (in_one_kernel(pages, blocks, step, most, items, 1)) return 256;
+  const int64_t rows = (int64_t)pages->n_layers * step->total_new * pages->n_kv_heads, stride = 16 * ((most_blocks(pages, blocks) + 15) / 16);
+  return align_up((size_t)(rows < 1 ? 1 : rows) * stride * sizeof(unsigned), 256);
 }
 
 extern "C" DAPQ_API int dapq_paged_select(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, const void* q, int32_t* idx,

@@ -12,6 +12,7 @@ struct SparsePlan {
   int64_t items;
   int parts, tiles;
 };
+int64_t resident_workgroups(const SparsePlan& plan) { return plan.cols == 32 ? 512 : 768; }
 SparsePlan sparse_plan(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step) {
   SparsePlan plan;
   const int group = step->n_q_heads / pages->n_kv_heads;
@@ -23,7 +24,7 @@ SparsePlan sparse_plan(const dapq_pages* pages, const dapq_blocks* blocks, const
   plan.tiles = (int)tiles;  // (up to 2^17: parts_each times it stays below 2^31)
   // Parts for as many workgroups as the chip holds at once, but of no fewer tiles than a workgroup has waves.  8 KV heads of one token, us with parts of
   // 2 / 4 / 8 tiles at least: 2048 rows of 4 query heads 9.8 / 9.3 / 10.5, of 8 query heads 10.2 / 10.2 / 11.4, 4096 rows 12.7 / 10.9 / 12.0.
-  const int64_t resident = plan.cols == 32 ? 512 : 768, items = plan.items * plan.chunks;
+  const int64_t resident = resident_workgroups(plan), items = plan.items * plan.chunks;
   int64_t parts = items > 0 ? resident / items : 1;
   if (parts > tiles / kRowWaves) parts = tiles / kRowWaves;
   plan.parts = (int)(parts < 1 ? 1 : parts);
@@ -75,8 +76,10 @@ using namespace dapq;
 
 extern "C" DAPQ_API size_t dapq_paged_sparse_attention_workspace_bytes(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step) {
   if (check_sparse(pages, blocks, step) != DAPQ_OK) return 0;
+  // Enough for every smaller step as well, which may share out its items where this one has enough of them.
   const SparsePlan plan = sparse_plan(pages, blocks, step);
-  return plan.parts > 1 ? align_up((size_t)plan.items * plan.chunks * plan.parts * plan.cols * (kHeadDim + 2) * sizeof(float), 256) : 256;
+  const int64_t parts_each = plan.tiles / kRowWaves, most = plan.items * plan.chunks * parts_each, resident = resident_workgroups(plan);
+  return parts_each > 1 ? align_up((size_t)(most < resident ? most : resident) * plan.cols * (kHeadDim + 2) * sizeof(float), 256) : 256;
 }
 
 extern "C" DAPQ_API int dapq_paged_sparse_attention(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, const void* q, const int32_t* idx,
