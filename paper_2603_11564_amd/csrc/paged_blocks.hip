@@ -440,8 +440,10 @@ __global__ __launch_bounds__(64 * WAVES) void paged_scores_kernel(SelectParams p
         i32x4 a[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) *reinterpret_cast<i32x4*>(turned + 1024 * i + 16 * lane) = tile.a[i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const i32x4*>(turned + 256 * n + (((4 * i + kg) ^ n) << 4));
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (the next tile goes through the same place)
         const bool plain = 16 * k >= middle0 && 16 * k + 16 <= middle1 && !__any(tile.scale < 0 || tile.scale == 255);
         float factor[4];  // of this lane's blocks
         const float mine = power_of_two(tile.scale < 0 ? 0 : tile.scale);
