@@ -308,7 +308,7 @@ int dapq_decode_attention(const dapq_shape* shape, const void* q_decode, const v
 enum { DAPQ_PAGES_BF16 = 0, DAPQ_PAGES_FP4 = 1, DAPQ_PAGES_E4M3 = 3 }; /* (2 is none) */
 typedef struct dapq_pages {
   int32_t n_layers;
-  int32_t batch;          /* sequences of the table; dapq_paged_gather and dapq_paged_read take up to 65535 */
+  int32_t batch;          /* sequences of the table; dapq_paged_gather, dapq_paged_read and dapq_paged_bounds take up to 65535 */
   int32_t n_kv_heads;
   int32_t head_dim;       /* 128 */
   int32_t format;         /* DAPQ_PAGES_* */
@@ -316,7 +316,7 @@ typedef struct dapq_pages {
   int32_t n_pages;        /* pages of a layer's pool */
   int32_t max_pages;      /* entries of a sequence in the table; max_pages * page_rows < 2^30 */
   void *k, *v;            /* device, the pools, 16-byte aligned */
-  void *k_scales, *v_scales;  /* device, 16-byte aligned; DAPQ_PAGES_FP4 only */
+  void *k_scales, *v_scales;  /* device, 16-byte aligned; DAPQ_PAGES_FP4 and DAPQ_PAGES_E4M3 */
   const int32_t* table;   /* device, [batch][max_pages] */
 } dapq_pages;
 
@@ -367,7 +367,8 @@ int dapq_paged_read(const dapq_pages* pages, const int32_t* lengths, int32_t max
  *   q    device, bf16, rotated, element (layer, token, head, c) by the q strides of step
  *   out  device, bf16 [n_layers][total_new][n_q_heads][128], 16-byte aligned; 0 where no row is visible
  *   workspace  device scratch of at least dapq_paged_attention_workspace_bytes(pages, step), 256-byte aligned: sums of cache parts that
- *        were shared out.  The figure depends on neither the lengths nor cu_new, so that a recorded call holds for all of them.
+ *        were shared out.  The figure depends on neither the lengths nor what cu_new holds, so that a recorded call holds for all of them; on whether cu_new is NULL it does (without it
+ *        a sequence has total_new / batch tokens, however large max_new is), and a step of fewer sequences or tokens, whose rows are shared out further, may need more.
  * Sums, maxima and weights are fp32.  Weights enter the product with the values as two bf16 numbers (the leading 16 bits of their significand, the others cut off) where
  * max_new x H_q/H_kv, the query rows of a KV head, is up to 32, and as one, rounded to nearest, beyond; the result is rounded once.
  * A column's sum of weighted values is taken before it is divided by the weights', each of which is up to 2^4: it may be infinite where 16 x rows x the largest
