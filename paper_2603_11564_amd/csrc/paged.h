@@ -35,8 +35,7 @@ constexpr int kBf16 = DAPQ_PAGES_BF16, kFp4 = DAPQ_PAGES_FP4, kE4m3 = DAPQ_PAGES
 constexpr int kRowBytes = 2 * kHeadDim;      // of a bf16 row
 template <int FMT>
 constexpr int kCodeBytes = FMT == kBf16 ? kRowBytes : (FMT == kFp4 ? kHeadDim / 2 : kHeadDim);  // of a row; codes have 4 scale bytes beside them
-template <int FMT>
-constexpr float kLargestScale = FMT == kFp4 ? 0x1p125f : 0x1p119f;  // of finite values: 6 * 2^125 and 448 * 2^119 are bf16 numbers, twice as much is not
+constexpr float kLargestFp4Scale = 0x1p125f;  // of finite values: 6 * 2^125 is a bf16 number, twice as much is not (E4M3: e4m3_past)
 constexpr unsigned kNoScale = 255;           // scale byte of a group with a value that is not finite
 // Bytes of a row with its scales (host).
 inline int row_bytes(const dapq_pages* p) {
@@ -105,7 +104,7 @@ __device__ __forceinline__ u32x4 fp4_unpack8(unsigned c, float s) {
 
 // Eight codes of FP4 of which those are 0 whose values with the scale s are no finite bf16: all of them without a scale, 2 and more at 2^127, 4 and 6 at 2^126.
 __device__ __forceinline__ unsigned fp4_finite8(unsigned c, float s) {
-  const unsigned past = s > 0x1p127f ? ~0u : (s > 0x1p126f ? c >> 2 : (s > kLargestScale<kFp4> ? c >> 2 & c >> 1 : 0u));  // (in the lowest bit of each code)
+  const unsigned past = s > 0x1p127f ? ~0u : (s > 0x1p126f ? c >> 2 : (s > kLargestFp4Scale ? c >> 2 & c >> 1 : 0u));  // (in the lowest bit of each code)
   return c & ~((past & 0x11111111u) * 15u);
 }
 

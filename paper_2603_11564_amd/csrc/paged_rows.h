@@ -448,7 +448,7 @@ __global__ __launch_bounds__(64 * kRowWaves, BLOCKS == 2 ? 2 : 3) void paged_row
             }
           }
         }
-        if (!SPARSE && __any(odd || top > kLargestScale<kFp4>)) {
+        if (!SPARSE && __any(odd || top > kLargestFp4Scale)) {
           if constexpr (FMT != kBf16) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
       float scale = group_scale(vs);
       bool past = false;
       if (loaded_row + (lane >> 2) >= seen_by_all) {
-        if constexpr (FMT == kFp4) past = scale > kLargestScale<kFp4>;
+        if constexpr (FMT == kFp4) past = scale > kLargestFp4Scale;
         else
 #pragma unroll
           for (int i = 0; i < 4 * kLoads; ++i) past |= e4m3_past(vr[i >> 2][i & 3], scale) != 0;
