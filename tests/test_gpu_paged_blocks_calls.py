@@ -60,3 +60,60 @@ def test_one_workspace_serves_steps_of_all_sizes():
         assert (np.abs(out.double().cpu().numpy() - exact) <= attention_bound(exact, weighted, size, 1)).all(), batch
         for work, n in zip(works, room):
             assert bool((work[n:] == 0xA5).all())
+
+
+# --- scores that tie --------------------------------------------------------------------------------------------------------
+LEVELS = [(150, 1), (150, 0), (120, 1), (120, 0)]     # scale byte, what the box of bounds is wider by: two pairs of close scores, the pairs far apart
+
+
+def tied_levels(rng, cache, b, q_bits, seq, blocks, shares):
+    """Bounds of a sequence's blocks 0 .. blocks - 1 that give its first token's queries one of four scores, wider boxes the higher ones: shares[i] blocks of level i, the last
+    of them all that are left, anywhere.  Returns the level of every block."""
+    level = np.full(blocks, len(LEVELS) - 1)
+    level[:sum(shares)] = np.repeat(np.arange(len(shares)), shares)
+    rng.shuffle(level)
+    group = q_bits.shape[2] // cache.heads
+    for head in range(cache.heads):
+        mid, half = rng.integers(-40, 41, 128), rng.integers(5, 31, 128)
+        step = np.ones(128, np.int64)
+        if group == 1:      # as close as two scores can be: one channel, of the least whole number of the query that is not 0
+            u, _ = BO.whole_query(O.bf16_bits_to_f64(q_bits[0, seq, head]))
+            step[:] = 0
+            step[np.argmin(np.where(u == 0, 1000, np.abs(u)))] = 1
+        for block in range(blocks):
+            page, row = divmod(block * b.block_rows, cache.page_rows)
+            at = (0, cache.table[seq, page], head, row // b.block_rows)
+            scale, wider = LEVELS[level[block]]
+            b.bounds[at][0], b.bounds[at][1], b.scales[at] = mid + half + wider * step, mid - half - wider * step, scale
+    return level
+
+
+@pytest.mark.parametrize("blocks,heads,sequences,group,new", [
+    (200, 2, 1, 1, 1), (256, 2, 3, 4, 1),           # one kernel of four waves
+    (400, 1, 1, 1, 1), (430, 2, 2, 8, 2),           # of eight
+    (2100, 8, 33, 1, 1),                            # of eight, four times four keys to a thread
+    (1000, 2, 2, 4, 3), (1000, 1, 1, 1, 1),         # chosen by a second kernel: up to 1024 blocks
+    (2000, 1, 1, 4, 1), (4000, 1, 1, 1, 1),         # 2048, 4096
+    (8100, 1, 1, 1, 1), (16000, 1, 1, 2, 1),        # 8192, 16384
+    (17000, 1, 1, 1, 1), (33000, 1, 2, 4, 1),       # any number, read from memory for every round
+])
+def test_ties_at_several_levels(blocks, heads, sequences, group, new):
+    """Blocks of four scores, with the last chosen one inside a level that others lie above: of it the first blocks are chosen."""
+    rng = np.random.default_rng(blocks)
+    lengths = [16 * blocks - 5 - new] + [int(n) for n in rng.integers(1, 300, sequences - 1)]
+    cache = Cache(rng, "bf16", 1, heads, 16, [n + new for n in lengths], extra_entries=0).to_device()
+    b = Bounds(cache, 16).random(rng)
+    q = normal_bits(rng, 1, sequences * new, heads * group, 128)
+    level = tied_levels(rng, cache, b, q, 0, blocks, (7, 20, 60))
+    b.to_device()
+    n_first, n_last = 2, 1
+    middle = level[n_first:blocks - n_last]
+    for cut in range(4):
+        above, of_cut = int((middle < cut).sum()), int((middle == cut).sum())
+        n_select = min(n_first + n_last + above + (of_cut + 1) // 2, 4096)
+        idx, count = check_choice(cache, b, lengths, [new] * sequences, q, n_select, n_first, n_last, ragged=False)
+        for head in range(heads):
+            assert count[0, new - 1, head] == n_select
+            chosen = np.isin(np.arange(blocks), idx[0, new - 1, head])[n_first:blocks - n_last]
+            assert chosen[middle < cut].all() and not chosen[middle > cut].any() and 0 < chosen[middle == cut].sum() < of_cut
+            assert np.array_equal(chosen[middle == cut], np.arange(of_cut) < chosen[middle == cut].sum())
