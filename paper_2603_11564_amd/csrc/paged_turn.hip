@@ -144,12 +144,13 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
     if constexpr (FMT != kBf16) {
       const int row = kTurnRows * wave + (lane >> 2);
       float scale = group_scale(vs);
-      bool past = false;
-      if (loaded_row + (lane >> 2) >= seen_by_all) {
-        if constexpr (FMT == kFp4) past = scale > kLargestFp4Scale;
-        else
+      bool past = loaded_row + (lane >> 2) >= seen_by_all;
+      if constexpr (FMT == kFp4) {
+        past = past && scale > kLargestFp4Scale;
+      } else if (past) {
+        past = false;
 #pragma unroll
-          for (int i = 0; i < 4 * kLoads; ++i) past |= e4m3_past(vr[i >> 2][i & 3], scale) != 0;
+        for (int i = 0; i < 4 * kLoads; ++i) past |= e4m3_past(vr[i >> 2][i & 3], scale) != 0;
       }
       if (past) {
         odd = true;
@@ -159,11 +160,12 @@ __global__ __launch_bounds__(64 * kTurnWaves, 8 / kTurnWaves) void paged_turn_ke
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        u32x4 k, v;
-        if constexpr (FMT == kFp4) k = fp4_unpack8(kr[0][i], group_scale(ks)), v = fp4_unpack8(vr[0][i], scale);
-        else k = e4m3_unpack8(kr[i >> 1][2 * (i & 1)], kr[i >> 1][2 * (i & 1) + 1], group_scale(ks)), v = e4m3_unpack8(vr[i >> 1][2 * (i & 1)], vr[i >> 1][2 * (i & 1) + 1], scale);
-        *reinterpret_cast<u32x4*>(kt + chunk_at(row, 4 * (lane & 3) + i)) = k;
-        *reinterpret_cast<u32x4*>(vt + chunk_at(row, 4 * (lane & 3) + i)) = v;
+        auto values = [&](const u32x4 (&codes)[kLoads], float s) {
+          if constexpr (FMT == kFp4) return fp4_unpack8(codes[0][i], s);
+          else return e4m3_unpack8(codes[i >> 1][2 * (i & 1)], codes[i >> 1][2 * (i & 1) + 1], s);
+        };
+        *reinterpret_cast<u32x4*>(kt + chunk_at(row, 4 * (lane & 3) + i)) = values(kr, group_scale(ks));
+        *reinterpret_cast<u32x4*>(vt + chunk_at(row, 4 * (lane & 3) + i)) = values(vr, scale);
       }
     } else {
 #pragma unroll
