@@ -429,7 +429,10 @@ int dapq_paged_bounds(const dapq_pages* pages, const dapq_blocks* blocks, const 
  *        token, KV head and block that the table has room for (a step of one token of 64 sequences, 8 KV heads, tables of 2048 blocks: 4 MB; 10000 tokens and 8192 blocks: 2.6 GB),
  *        or 256 bytes where no step of that size needs it.  The figure depends on neither the lengths nor cu_new, be it NULL or not, and is enough for every step of
  *        no more sequences, layers, KV heads and new tokens (total_new and max_new), and tables no wider, with as many query heads a KV head.
- * Uses the table of pages, all of blocks, and n_q_heads, max_new, total_new, cu_new, lengths and the q strides of step. */
+ * Uses the table of pages, all of blocks, and n_q_heads, max_new, total_new, cu_new, lengths and the q strides of step.
+ * How blocks are shared out over the chip is decided by the table's width and the number of sequences, not by their lengths: one sequence of 131000 rows among 63 of 1000 in
+ * blocks of 16, 8 KV heads, takes 54 us in one call, and 17 and 6 in two.
+ * A turn of a prompt's size is better cut into calls of some hundred tokens, which the same workspace serves one after the other. */
 int dapq_paged_select(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, const void* q, int32_t* idx, int32_t* count,
                       void* workspace, size_t workspace_bytes, void* stream);
 

@@ -17,7 +17,7 @@ RowPlan row_plan(const dapq_pages* p, int cols) {
   // of the chip.  Us, parts / items, 8 KV heads, bf16, sequences x rows: 1 x 600 10.6 / 9.7, 1 x 1000 11.9 / 13.6, 1 x 8000 17.2 / 74.3, 4 x 1000 13.0 / 14.2,
   // 8 x 1000 15.0 / 14.4, 8 x 2000 19.4 / 22.7, 16 x 2000 34.0 / 30.0, 16 x 4000 57.5 / 55.5, 24 x 2000 47 / 37; in 4 bits 1 x 1000 11.3 / 9.8, 1 x 2000
   // 11.5 / 15.2, 8 x 1000 12.2 / 10.0, 8 x 2000 13.7 / 15.4, 16 x 2000 16.3 / 15.6, 16 x 4000 21.2 / 26.3, 31 x 2000 20.8 / 16.2.
-  // In 8 bits 1 x 1000 10.9 / 10.7, 1 x 2000 10.8 / 16.7, 4 x 1000 12.3 / 10.8, 8 x 2000 15.9 / 18.0, 16 x 2000 20.5 / 18.3, 16 x 4000 30.7 / 35.7, 31 x 2000 28.1 / 22.4.
+  // (In 8 bits an item alone takes 0.19 a tile, but then 16 x 4000 would be items.)  In 8 bits 1 x 1000 10.9 / 10.7, 1 x 2000 10.8 / 16.7, 4 x 1000 12.3 / 10.8, 8 x 2000 15.9 / 18.0, 16 x 2000 20.5 / 18.3, 16 x 4000 30.7 / 35.7, 31 x 2000 28.1 / 22.4.
   const bool fp4 = p->format == DAPQ_PAGES_FP4, e4m3 = p->format == DAPQ_PAGES_E4M3;
   const double tile = fp4 ? 0.16 : (e4m3 ? 0.22 : 0.27), bytes = (fp4 ? 4352 : (e4m3 ? 8448 : 16384)) / 6.5e6, join = fp4 ? 6.5 : (e4m3 ? 6.0 : 5.5);
   // Lengths are not known here, only the table's width: from 30 us an item on parts also keep a long sequence from outlasting the others (8 KV heads, bf16, 16

@@ -615,6 +615,8 @@ int64_t column_tiles(int group, int cols_log2, int64_t most) {
 // some 3 us.  With several column tiles every workgroup reads the bounds, which pays while they are few.  Us, one kernel / two, 8 KV heads, 4 query heads a KV head, sequences x blocks: 1 x 128 6.5 / 8.9, 1 x 512 8.9 / 9.1, 1 x 2048 20.0 / 9.4, 8 x 512 9.1 / 9.8,
 // 16 x 2048 20.9 / 21.4, 16 x 256..8192 65 / 42, 32 x 1024 16.0 / 20.5, 64 x 512 16.6 / 20.9, 64 x 2048 53 / 64, two tokens of 64 x 256 15.0 / 16.2; 8 query heads, four tokens of 16 x 512 12.3 /
 // 13.5, of 64 x 64 11.2 / 14.6, of 64 x 256 25.4 / 18.1, eight of 64 x 64 18.5 / 21.0; 16 query heads, two tokens of 16 x 512 9.8 / 13.0, four of 32 x 512..2048 50 / 32.
+// Lengths are not known here: one sequence that fills a table of 2048 / 4096 / 8192 blocks among 63 of 63 blocks 17.7 / 21.0, 30.7 / 34.1, 53.8 / 57.2 (in calls of their own 10.9, 13.7, 17.4
+// and 6.0).  Its blocks are one workgroup's in either form, since chunks are cut for as many long sequences as there are; the second kernel is 3 us behind here too.
 // fewest: the items; or 1, to ask whether calls of fewer items are one kernel as well (fewer tokens and items meet all other conditions too).
 bool in_one_kernel(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, int64_t most, int64_t items, int64_t fewest) {
   const int cols_log2 = columns_log2(pages, step);
@@ -695,6 +697,9 @@ extern "C" DAPQ_API int dapq_paged_bounds(const dapq_pages* pages, const dapq_bl
   const int64_t all = most_blocks(pages, blocks), most = ((int64_t)max_rows + blocks->block_rows - 1) / blocks->block_rows;
   // 8 layers of 32768 rows, us, a block of 16 rows shared by a wave / not, of 32, of 64: bf16 106 / 113, 101 / 108, 99 / 99; in 8 bits 85 / 62, 69 / 65, 58 / 57; in 4 bits
   // 78 / 42, 53 / 35, 42 / 32, but 64 blocks of 64 rows 4.2 / 6.6.  In bf16 bytes bound both, and rows that follow each other are read at once by the first.
+  // Of 128 rows, the same call repeated, 43 / 45 in 8 bits and 34 / 29 in 4, of 256 43 / 42 and 32 / 32; one layer of them 8.1 / 14.0, 6.4 / 10.0 and 10.9 / 24.8, 7.3 / 17.7.  A token
+  // of 64 sequences, 16 / 32 / 64 / 128 / 256 rows: 3.2 / 4.6, 3.4 / 6.2, 4.1 / 9.6, 5.1 / 16.5, 7.4 / 30.  Above 32 rows the shared form is never far behind and far ahead where blocks are
+  // few; below, the other one wins with many blocks and loses up to 3 us with few.  The rule knows no number of blocks, so that in 4 bits many blocks of 64 pay a third more.
   const bool shared = pages->format == DAPQ_PAGES_BF16 || blocks->block_rows > 32;
   const int of_group = shared ? 4 : 16;  // blocks
   const int64_t groups = ((most < all ? most : all) + of_group - 1) / of_group;

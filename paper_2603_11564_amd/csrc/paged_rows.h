@@ -97,7 +97,7 @@ struct Part {
 //            step of the result.  A third number would be another product for every eight channels where columns exceed 8.
 //            V is transposed in registers: a lane loads the same 8 channels of 8 rows.
 // Bound by bytes where there are enough items: bf16, 256 sequences of 1000 rows, 8 KV heads 182 us (5.8 TB/s), in 4 bits 55 (5.1 TB/s, where 335 vector
-// instructions a tile begin to count: three waves to a SIMD, two take 63); one item alone takes 0.27 us a tile in bf16, 0.16 in 4 bits, behind 5 to 6 us.  In 8 bits 64
+// instructions a tile begin to count: three waves to a SIMD, two take 63); one item alone takes 0.27 us a tile in bf16, 0.17 in 4 bits, behind 5 to 6 us.  In 8 bits 64
 // sequences of 4000 rows 94 us (5.8 TB/s), 0.19 us a tile.
 // BLOCKS: blocks of 16 columns; 0: up to 8 columns, whose leading and following parts take the two halves of one block.
 // SPLIT: a workgroup has a part of an item; else an item (and nothing is to be joined).
