@@ -432,7 +432,7 @@ int dapq_paged_bounds(const dapq_pages* pages, const dapq_blocks* blocks, const 
  * Uses the table of pages, all of blocks, and n_q_heads, max_new, total_new, cu_new, lengths and the q strides of step.
  * How blocks are shared out over the chip is decided by the table's width and the number of sequences, not by their lengths: one sequence of 131000 rows among 63 of 1000 in
  * blocks of 16, 8 KV heads, takes 54 us in one call, and 17 and 6 in two.
- * A turn of a prompt's size is better cut into calls of some hundred tokens, which the same workspace serves one after the other. */
+ * A turn of a prompt's size is better cut into calls of some hundred tokens, one after the other on one stream with one workspace. */
 int dapq_paged_select(const dapq_pages* pages, const dapq_blocks* blocks, const dapq_step* step, const void* q, int32_t* idx, int32_t* count,
                       void* workspace, size_t workspace_bytes, void* stream);
 
@@ -443,8 +443,8 @@ size_t dapq_paged_select_workspace_bytes(const dapq_pages* pages, const dapq_blo
  * of the blocks idx[layer][cu_new[seq] + t][kv_head][0 .. count - 1], in the format of dapq_paged_select.  An entry that is no block of the table has no rows;
  * blocks may stand in any order, and one that is named twice counts twice.  A count past n_select counts as n_select, a negative one as 0.
  *   q, out     as for dapq_paged_attention; 0 where no row is visible
- *   workspace  device scratch of at least dapq_paged_sparse_attention_workspace_bytes(pages, blocks, step), 256-byte aligned; up to 8.5 MB.  The figure holds for
- *        smaller steps as that of dapq_paged_select does
+ *   workspace  device scratch of at least dapq_paged_sparse_attention_workspace_bytes(pages, blocks, step), 256-byte aligned; up to 8.5 MB.  The figure is
+ *        enough for the smaller steps that dapq_paged_select's is enough for, with no more blocks to choose
  * Uses block_rows and n_select of blocks (bounds and scales may be NULL), and what dapq_paged_attention uses of step, softcap too.  Sums, weights
  * and values that are not finite are as in dapq_paged_attention of few query rows.  The work is that of the chosen rows, read anew for every token: a
  * turn of many tokens behind a cache that is not many times longer than n_select * block_rows is done sooner by dapq_paged_attention (200 tokens over 64 blocks of 16
